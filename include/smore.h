@@ -346,6 +346,173 @@ int smore_wait_before_kernel(void *event, int32_t which);
 int smore_gather_probe(const void *table, int64_t table_bytes, int64_t n_reads, uint32_t *sink,
                        int64_t sink_words, void *hip_stream);
 
+/* ---------------------------------------------------------------------
+   Training on sampled batches: candidate scores, the preference loss of a
+   positive against its verified negatives, and AdamW.  Like the sampling
+   calls they validate on the host, launch on hip_stream and return; the
+   device of the buffers must be the current one.  Strides count elements.
+   Rows of any length and any alignment of a whole element are accepted.
+   Sums are in fp32 in a fixed order: equal calls give equal bits. */
+
+/* element types */
+enum { SMORE_F32 = 0, SMORE_BF16 = 1, SMORE_F16 = 2 };
+
+/* Sizes of smore_score / smore_score_grad.
+   batch B (>= 1), n candidates per query (>= 0), dim (1 .. 2^20);
+   n_rows        rows V of the table (>= 1)
+   table_stride, query_stride (>= dim), candidate_stride, score_stride
+                 (>= n): distance of two rows; the rows of the candidates
+                 may coincide (candidate_stride 0: one set for all queries)
+   table_type, query_type  SMORE_F32 or SMORE_BF16 */
+typedef struct {
+    int32_t batch, n, dim, n_rows;
+    int64_t table_stride, query_stride, candidate_stride, score_stride;
+    int32_t table_type, query_type;
+} smore_score_args;
+
+/* scores [B, n] (fp32): the product of each query's vector (queries
+   [B, dim]) with the table rows (table [V, dim]) of its candidates (int32
+   [B, n], as smore_sample writes them).  A candidate outside [0, V), such
+   as the -1 of a short row, has score 0 and reads no row.  Errors:
+   SMORE_E_INVALID_ARG, SMORE_E_UNSUPPORTED for another type,
+   SMORE_E_OVERFLOW when B x ceil(n / 8) reaches 2^26. */
+int smore_score(const smore_score_args *args, const void *table, const void *queries,
+                const int32_t *candidates, float *scores, void *hip_stream);
+
+/* Gradient of smore_score for the queries: grad_queries [B, dim] (of
+   query_type, strides query_stride) = sum over k of grad_scores [B, n]
+   (fp32, strides score_stride) times the row of candidate k.  Candidates
+   outside [0, V) add nothing, whatever their grad_scores hold; n = 0 gives
+   zeros.  Few queries with long lists are split over the chip and need a
+   workspace (smore_score_grad_workspace_bytes, 0 where they are not; scratch
+   after the call, not shared by calls that overlap).  The gradient for the
+   table is taken by smore_adamw, row by row.  B below 2^24, else
+   SMORE_E_OVERFLOW. */
+int smore_score_grad_workspace_bytes(const smore_score_args *args, size_t *bytes);
+int smore_score_grad(const smore_score_args *args, const void *table, const int32_t *candidates,
+                     const float *grad_scores, void *grad_queries, void *workspace,
+                     size_t ws_bytes, void *hip_stream);
+
+/* Preference loss of paired log ratios.  For row b and its valid negatives
+   k (c of them)
+       z_k = beta ((positive - ref_positive) - (negatives[k] - ref_negatives[k]))
+   SMORE_PREFERENCE_PAIRS    loss = 1/c sum_k (1 - smoothing) softplus(-z_k)
+                                             + smoothing softplus(z_k)
+   SMORE_PREFERENCE_SOFTMAX  loss = log(1 + sum_k exp(-z_k)), all negatives
+                             against the positive at once (smoothing 0)
+   With scores that are log probabilities up to a constant of the row the
+   constant cancels. */
+enum { SMORE_PREFERENCE_PAIRS = 0, SMORE_PREFERENCE_SOFTMAX = 1 };
+
+/* batch B (>= 1, below 2^24), n negatives per row (0 .. 2^30), kind, score_type
+   (SMORE_F32, _BF16, _F16: of the scores, the reference scores and the
+   gradients), beta (finite, > 0), smoothing ([0, 1)), scale (finite: factor
+   of the gradients), and the distances (>= 0) of two rows of each array; rows
+   of the gradients must not overlap. */
+typedef struct {
+    int32_t batch, n, kind, score_type;
+    float beta, smoothing, scale;
+    int64_t positive_stride, negatives_stride, ref_positive_stride, ref_negatives_stride,
+        grad_positive_stride, grad_negatives_stride;
+} smore_preference_args;
+
+/* positive [B], negatives [B, n]; ref_positive, ref_negatives the same of the
+   reference model, both NULL for none.  Valid negatives of row b: the first
+   n_valid[b] (int32 [B], as smore_sample writes it; -1 and 0: none, more
+   than n: n), or those with bit k % 32 of word k / 32 of row b of mask set
+   (uint32 [B, (n + 31) / 32], as smore_sample_shared and smore_verify write
+   it), or all n where both are NULL; not both.  weight (fp32 [B] or NULL):
+   factor of each row's gradient. */
+typedef struct {
+    const void *positive, *negatives, *ref_positive, *ref_negatives;
+    const int32_t *n_valid;
+    const uint32_t *mask;
+    const float *weight;
+} smore_preference_in;
+
+/* loss [B] (fp32, unweighted; NULL: not wanted), and scale x weight[b] times
+   the gradient of row b's loss: grad_positive [B], grad_negatives [B, n]
+   (both NULL: not wanted).  A row without a valid negative has loss and
+   gradients 0; places that are not valid are not used and get gradient 0.
+   A valid score that is NaN makes its row NaN, as in the formula.  Outputs
+   must not overlap inputs or each other. */
+typedef struct {
+    float *loss;
+    void *grad_positive, *grad_negatives;
+} smore_preference_out;
+
+int smore_preference_loss(const smore_preference_args *args, const smore_preference_in *in,
+                          const smore_preference_out *out, void *hip_stream);
+
+/* AdamW with decoupled weight decay, for many tensors in one call:
+       m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+       p = p (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+   Arithmetic is in fp32.
+
+   A dense tensor (rows NULL) has n_rows x dim elements in a row, and so have
+   its gradient and its moments.  A table (rows given) is stepped only in the
+   rows that a batch touched: rows (int32 [n_entries], ascending, repeats
+   allowed) names a row per entry, and the gradient of a row is the sum over
+   its entries i of coef[o] x grad[o / per], o = order[i], where grad is
+   [ceil(n_entries / per), dim], order (int64) is a permutation of the
+   entries (NULL: o = i) and coef is fp32 (NULL: 1).  With ids, grad_scores
+   and queries of smore_score flattened and sorted by id, per = n, this is
+   smore_score's gradient for the table, never written out.  Entries outside
+   [0, n_rows) are skipped; all other rows keep their values and moments,
+   without decay.
+
+   bits 32: m, v fp32.  bits 8: m and v are bytes, e4m3 codes of m and of
+   sqrt(v) divided by the scale of their block of SMORE_ADAMW_BLOCK
+   consecutive elements of a row (a dense tensor is one row): m_scale,
+   v_scale fp32, [ceil(elements / block)], for tables [n_rows,
+   ceil(dim / block)].  Moments that are all zero bytes are moments 0.
+   A moment that is not finite makes its block NaN.
+
+   SMORE_ADAMW_STOCHASTIC: codes and bf16 parameters are rounded up or down
+   at random by their remainder (nearest, ties to even, without it), from a
+   hash of (seed, t, index, position): a step that is run again from the same
+   values gives the same bits.  index tells the tensors of a model apart. */
+#define SMORE_ADAMW_BLOCK 128
+#define SMORE_ADAMW_STOCHASTIC 1u
+
+typedef struct {
+    void *param;        /* SMORE_F32 or SMORE_BF16 */
+    const void *grad;   /* SMORE_F32, _BF16 or _F16 */
+    void *m, *v;
+    float *m_scale, *v_scale;
+    const int32_t *rows;
+    const int64_t *order;
+    const float *coef;
+    int64_t n_rows, dim, n_entries, per;
+    int32_t param_type, grad_type, bits, index;
+    float weight_decay;
+} smore_adamw_tensor;
+
+/* lr (finite, >= 0), beta1, beta2 in [0, 1), eps (finite, >= 0), step t (>= 1).
+   On the device, for steps captured into a graph (NULL: not used):
+   step_device (int64, >= 1) and lr_device (fp32) replace step and lr;
+   grad_scale (fp32) multiplies every gradient, and where it is not finite
+   nothing is written. */
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    const int64_t *step_device;
+    const float *lr_device;
+    const float *grad_scale;
+    uint64_t seed;
+    uint32_t flags;
+} smore_adamw_args;
+
+/* Steps n_tensors (host array) tensors.  Parameters and moments must not
+   overlap, neither within a tensor nor between tensors: of the parameters
+   this is checked (SMORE_E_INVALID_ARG).  The workspace holds sums of long
+   runs of equal rows (0 bytes without tables; scratch after the call, not
+   shared by calls that overlap).  SMORE_E_OVERFLOW: 2^26 or more entries, or
+   2^34 or more elements. */
+int smore_adamw_workspace_bytes(const smore_adamw_tensor *tensors, int32_t n_tensors, size_t *bytes);
+int smore_adamw(const smore_adamw_tensor *tensors, int32_t n_tensors, const smore_adamw_args *args,
+                void *workspace, size_t ws_bytes, void *hip_stream);
+
 /* Release a graph (NULL is a no-op). */
 void smore_free_graph(smore_graph *g);
 

@@ -57,6 +57,49 @@ OUT_FIELDS = ("anchors", "relations", "positive", "negatives", "n_valid", "pos_a
               "neg_draws")
 
 
+F32, BF16, F16 = range(3)
+PREFERENCE_KINDS = {"pairs": 0, "softmax": 1}
+ADAMW_BLOCK = 128
+ADAMW_STOCHASTIC = 1
+
+
+class ScoreArgs(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("n", c_i32), ("dim", c_i32), ("n_rows", c_i32),
+                ("table_stride", c_i64), ("query_stride", c_i64), ("candidate_stride", c_i64),
+                ("score_stride", c_i64), ("table_type", c_i32), ("query_type", c_i32)]
+
+
+class PreferenceArgs(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("n", c_i32), ("kind", c_i32), ("score_type", c_i32),
+                ("beta", ctypes.c_float), ("smoothing", ctypes.c_float), ("scale", ctypes.c_float),
+                ("positive_stride", c_i64), ("negatives_stride", c_i64),
+                ("ref_positive_stride", c_i64), ("ref_negatives_stride", c_i64),
+                ("grad_positive_stride", c_i64), ("grad_negatives_stride", c_i64)]
+
+
+class PreferenceIn(ctypes.Structure):
+    _fields_ = [(n, c_vp) for n in ("positive", "negatives", "ref_positive", "ref_negatives",
+                                    "n_valid", "mask", "weight")]
+
+
+class PreferenceOut(ctypes.Structure):
+    _fields_ = [(n, c_vp) for n in ("loss", "grad_positive", "grad_negatives")]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [(n, c_vp) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "rows",
+                                    "order", "coef")] + \
+               [(n, c_i64) for n in ("n_rows", "dim", "n_entries", "per")] + \
+               [(n, c_i32) for n in ("param_type", "grad_type", "bits", "index")] + \
+               [("weight_decay", ctypes.c_float)]
+
+
+class AdamWArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps")] + \
+               [("step", c_i64), ("step_device", c_vp), ("lr_device", c_vp), ("grad_scale", c_vp),
+                ("seed", c_u64), ("flags", c_u32)]
+
+
 class SmoreError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{ERRORS.get(code, code)}: {msg}")
@@ -104,6 +147,17 @@ def lib() -> ctypes.CDLL:
         L.smore_profile_kernel.argtypes = [c_vp, c_vp, c_i32]
         L.smore_wait_before_kernel.argtypes = [c_vp, c_i32]
         L.smore_gather_probe.argtypes = [c_vp, c_i64, c_i64, c_vp, c_i64, c_vp]
+        sp = ctypes.POINTER(ctypes.c_size_t)
+        L.smore_score.argtypes = [ctypes.POINTER(ScoreArgs)] + [c_vp] * 5
+        L.smore_score_grad_workspace_bytes.argtypes = [ctypes.POINTER(ScoreArgs), sp]
+        L.smore_score_grad.argtypes = [ctypes.POINTER(ScoreArgs)] + [c_vp] * 5 + [ctypes.c_size_t,
+                                                                                  c_vp]
+        L.smore_preference_loss.argtypes = [ctypes.POINTER(PreferenceArgs),
+                                            ctypes.POINTER(PreferenceIn),
+                                            ctypes.POINTER(PreferenceOut), c_vp]
+        L.smore_adamw_workspace_bytes.argtypes = [c_vp, c_i32, sp]
+        L.smore_adamw.argtypes = [c_vp, c_i32, ctypes.POINTER(AdamWArgs), c_vp, ctypes.c_size_t,
+                                  c_vp]
         L.smore_free_graph.argtypes = [c_vp]
         L.smore_free_graph.restype = None
         _lib = L
@@ -448,3 +502,392 @@ def gather_probe(table, n_reads: int, stream=None):
     _check(lib().smore_gather_probe(c_vp(table.data_ptr()), table.numel() * table.element_size(),
                                     n_reads, c_vp(sink.data_ptr()), threads, c_vp(st.cuda_stream)))
     return sink
+
+
+# ------------------------------------------------- training on sampled batches
+def _types() -> dict:
+    import torch
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+class _Launch:
+    """The device of a call's tensors made current, and its stream: the given
+    one, or the device's current stream.  Tensors made inside belong to that
+    stream."""
+
+    def __init__(self, device, stream):
+        import torch
+        if device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, not on {device}")
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        self._guard = None
+        if stream is not None:
+            self._guard = torch.cuda.stream(stream)
+        elif torch.cuda.current_device() != device.index:
+            self._guard = torch.cuda.device(device)
+        self.handle = c_vp((stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream)
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+        return self.handle
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _operand(name: str, t, shape: tuple, dtypes, device) -> None:
+    """A device tensor of this shape and one of these types whose rows are
+    contiguous (the distance of two rows is free)."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if t.device != device or t.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU of the other tensors ({device}), it is on {t.device}")
+    if len(shape) == 2 and shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"rows of {name} must be contiguous")
+
+
+def _pitch(t) -> int:
+    """Distance of two rows of a matrix (a length for a single row)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None and t.numel() else None
+
+
+def _score_args(table, candidates, query_type, query_pitch: int, score_pitch: int) -> ScoreArgs:
+    v, dim = table.shape
+    batch, n = candidates.shape
+    # one set for all queries: rows that coincide
+    pitch = candidates.stride(0) if batch > 1 else 0
+    return ScoreArgs(batch, n, dim, v, _pitch(table), query_pitch, pitch, score_pitch,
+                     _types()[table.dtype], _types()[query_type])
+
+
+def _check_table(table, candidates) -> None:
+    import torch
+    if table.dim() != 2 or candidates.dim() != 2:
+        raise ValueError("table and candidates must be matrices")
+    wide = (torch.float32, torch.bfloat16)
+    _operand("table", table, tuple(table.shape), wide, table.device)
+    _operand("candidates", candidates, tuple(candidates.shape), (torch.int32,), table.device)
+
+
+def score_into(table, queries, candidates, scores, stream=None):
+    """smore_score into the caller's fp32 tensor [batch, n]."""
+    import torch
+    _check_table(table, candidates)
+    _operand("queries", queries, (candidates.shape[0], table.shape[1]), (torch.float32, torch.bfloat16), table.device)
+    _operand("scores", scores, tuple(candidates.shape), (torch.float32,), table.device)
+    args = _score_args(table, candidates, queries.dtype, _pitch(queries), _pitch(scores))
+    with _Launch(table.device, stream) as st:
+        _check(lib().smore_score(ctypes.byref(args), _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st))
+    return scores
+
+
+def score(table, queries, candidates, stream=None):
+    """Scores (fp32 [batch, n]) of each query's candidates (int32 [batch, n], as
+    sampled): the product of queries [batch, dim] with the candidates' rows of
+    table [V, dim], 0 for candidates outside [0, V) (smore_score).  For one
+    candidate set shared by all queries, candidates.expand(batch, n) works,
+    but a matrix product with the set's rows is the faster way."""
+    import torch
+    with _Launch(table.device, stream):
+        scores = torch.empty(tuple(candidates.shape), dtype=torch.float32, device=table.device)
+    return score_into(table, queries, candidates, scores, stream)
+
+
+def score_grad_into(table, candidates, grad_scores, grad_queries, stream=None):
+    """smore_score_grad into the caller's tensor [batch, dim]."""
+    import torch
+    _check_table(table, candidates)
+    batch = candidates.shape[0]
+    _operand("grad_scores", grad_scores, tuple(candidates.shape), (torch.float32,), table.device)
+    _operand("grad_queries", grad_queries, (batch, table.shape[1]), (torch.float32, torch.bfloat16), table.device)
+    args = _score_args(table, candidates, grad_queries.dtype, _pitch(grad_queries), _pitch(grad_scores))
+    need = ctypes.c_size_t()
+    _check(lib().smore_score_grad_workspace_bytes(ctypes.byref(args), ctypes.byref(need)))
+    with _Launch(table.device, stream) as st:
+        # of this call alone, from the stream's (or the capturing graph's) memory
+        ws = torch.empty(need.value, dtype=torch.uint8, device=table.device) if need.value else None
+        _check(lib().smore_score_grad(ctypes.byref(args), _ptr(table), _ptr(candidates), _ptr(grad_scores),
+                                      _ptr(grad_queries), _ptr(ws), need.value, st))
+    return grad_queries
+
+
+def score_grad(table, candidates, grad_scores, dtype=None, stream=None):
+    """Gradient of score() for the queries, [batch, dim] in dtype (fp32): the
+    sum of the candidates' rows, each times its entry of grad_scores (fp32
+    [batch, n]).  The gradient for the table is AdamW's: row_grad()."""
+    import torch
+    with _Launch(table.device, stream):
+        out = torch.empty((candidates.shape[0], table.shape[1]), dtype=dtype or torch.float32, device=table.device)
+    return score_grad_into(table, candidates, grad_scores, out, stream)
+
+
+def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_negatives=None, n_valid=None,
+                         mask=None, kind: str = "pairs", beta: float = 0.1, smoothing: float = 0.0, weight=None,
+                         stream=None) -> dict:
+    """smore_preference_loss into the caller's tensors: out has "loss" (fp32
+    [batch]), or "grad_positive" [batch] and "grad_negatives" [batch, n] of
+    the scores' type, or all three."""
+    import torch
+    if kind not in PREFERENCE_KINDS:
+        raise ValueError(f"kind must be one of {sorted(PREFERENCE_KINDS)}, got {kind!r}")
+    if negatives.dim() != 2:
+        raise ValueError("negatives must be a matrix")
+    batch, n = negatives.shape
+    device, dtype = negatives.device, negatives.dtype
+    if dtype not in _types():
+        raise ValueError(f"scores must be fp32, bf16 or fp16, got {dtype}")
+    if (ref_positive is None) != (ref_negatives is None):
+        raise ValueError("reference scores are given for both, or for neither")
+    grads = [out.get("grad_positive"), out.get("grad_negatives")]
+    if (grads[0] is None) != (grads[1] is None):
+        raise ValueError("gradients are wanted for both, or for neither")
+    for name, t, shape, types in (("positive", positive, (batch,), (dtype,)), ("negatives", negatives, (batch, n), (dtype,)),
+                                  ("ref_positive", ref_positive, (batch,), (dtype,)),
+                                  ("ref_negatives", ref_negatives, (batch, n), (dtype,)),
+                                  ("n_valid", n_valid, (batch,), (torch.int32,)),
+                                  ("mask", mask, (batch, (n + 31) // 32), (torch.int32,)),
+                                  ("loss", out.get("loss"), (batch,), (torch.float32,)),
+                                  ("grad_positive", grads[0], (batch,), (dtype,)),
+                                  ("grad_negatives", grads[1], (batch, n), (dtype,))):
+        if t is not None:
+            _operand(name, t, shape, types, device)
+    scale = 1.0
+    if weight is not None and not isinstance(weight, torch.Tensor):
+        scale, weight = float(weight), None
+    if weight is not None:
+        _operand("weight", weight, (batch,), (torch.float32,), device)
+    for name, t in (("n_valid", n_valid), ("mask", mask), ("weight", weight), ("loss", out.get("loss"))):
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    row = lambda t: 0 if t is None else t.stride(0) if batch > 1 else n
+    args = PreferenceArgs(batch, n, PREFERENCE_KINDS[kind], _types()[dtype], beta, smoothing, scale, row(positive),
+                          row(negatives), row(ref_positive), row(ref_negatives), row(grads[0]), row(grads[1]))
+    ins = PreferenceIn(*[_ptr(t) for t in (positive, negatives, ref_positive, ref_negatives, n_valid, mask, weight)])
+    outs = PreferenceOut(*[_ptr(t) for t in (out.get("loss"), *grads)])
+    with _Launch(device, stream) as st:
+        _check(lib().smore_preference_loss(ctypes.byref(args), ctypes.byref(ins), ctypes.byref(outs), st))
+    return out
+
+
+def preference_loss(positive, negatives, ref_positive=None, ref_negatives=None, n_valid=None, mask=None,
+                    kind: str = "pairs", beta: float = 0.1, smoothing: float = 0.0, weight=None, grad: bool = True,
+                    stream=None) -> dict:
+    """Preference loss of each query's positive (scores [batch]) against its
+    verified negatives (scores [batch, n]), optionally relative to a reference
+    model's scores: {"loss" (fp32 [batch])}, with grad also {"grad_positive",
+    "grad_negatives"}, the gradient of the sum of weight (a number or fp32
+    [batch], default 1) times loss.  Which negatives count: n_valid as
+    sample() gives it, or mask as sample_shared() and verify() give it.  kind
+    "pairs" averages the paired losses, with label smoothing; "softmax"
+    takes the positive against all negatives at once.  The formulas stand at
+    smore_preference_loss.  Scores may be views of one matrix (a column, the
+    columns behind it)."""
+    import torch
+    with _Launch(negatives.device, stream):
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=negatives.device)
+        out = {"loss": new(negatives.shape[:1], torch.float32)}
+        if grad:
+            out["grad_positive"] = new(negatives.shape[:1], negatives.dtype)
+            out["grad_negatives"] = new(tuple(negatives.shape), negatives.dtype)
+    return preference_loss_into(positive, negatives, out, ref_positive, ref_negatives, n_valid, mask, kind, beta,
+                                smoothing, weight, stream)
+
+
+class RowGrad:
+    """The gradient of a table in the rows that a batch touched: entry i of
+    rows (int32, ascending, repeats allowed) adds coef[o] times
+    grad[o // per], o = order[i], to its row (order int64 and coef fp32 by
+    entry, both optional).  Entries outside the table are skipped."""
+
+    def __init__(self, rows, grad, order=None, coef=None, per: int = 1):
+        self.rows, self.grad, self.order, self.coef, self.per = rows, grad, order, coef, per
+
+
+def row_grad(ids, grad, coef=None, per: int = 1) -> RowGrad:
+    """RowGrad of ids in any order and shape (int32): entry i, counted over
+    the flattened ids, adds coef[i] times grad[i // per].  With score()'s
+    candidates [batch, n] as ids, its queries as grad, the gradient of its
+    scores as coef and per = n this is score()'s gradient for the table."""
+    import torch
+    rows, order = torch.sort(ids.reshape(-1), stable=True)
+    return RowGrad(rows, grad, order, None if coef is None else coef.reshape(-1), per)
+
+
+def alloc_adamw_state(param, bits: int = 32, table: bool = False) -> dict:
+    """Zero moments of a parameter: {"m", "v"}, fp32 of its shape, or in 8
+    bits float8_e4m3fn codes of m and sqrt(v) with fp32 scales "m_scale",
+    "v_scale" per block of ADAMW_BLOCK elements: of each row for a table
+    [V, dim] whose rows are stepped, else of the parameter as one row."""
+    import torch
+    new = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=param.device)
+    if bits == 32:
+        return {k: new(tuple(param.shape), torch.float32) for k in ("m", "v")}
+    if bits != 8:
+        raise ValueError(f"moments have 8 or 32 bits, not {bits}")
+    blocks = lambda n: -(-n // ADAMW_BLOCK)
+    shape = (param.shape[0], blocks(param.shape[1])) if table else (blocks(param.numel()),)
+    state = {k: new(tuple(param.shape), torch.uint8).view(torch.float8_e4m3fn) for k in ("m", "v")}
+    state.update({k: new(shape, torch.float32) for k in ("m_scale", "v_scale")})
+    return state
+
+
+class AdamW:
+    """AdamW (smore_adamw) over a list of parameters (fp32 or bf16), with
+    moments in 32 or 8 bits.
+
+    tables: numbers of the parameters that are tables [V, dim] stepped by
+    rows (RowGrad).  states: their moments as alloc_adamw_state makes them,
+    e.g. of a checkpoint (they are used, not copied), steps the steps taken.
+    seed: roundings to 8 bits and to bf16 are stochastic, keyed by it (None:
+    to the nearest).  lr: a number, or an fp32 device tensor [1].  device_step:
+    the step count is kept in an int64 device tensor, counted up by a kernel,
+    so that a captured step counts when it is replayed.
+
+    Moments are in .states, the count in .steps (.device_steps)."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                 bits: int = 32, seed: "int | None" = None, tables=(), states=None, steps: int = 0,
+                 device_step: bool = False):
+        import torch
+        self.params = list(params)
+        self.lr, self.betas, self.eps, self.seed, self.steps = lr, betas, eps, seed, steps
+        self.weight_decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else \
+            [weight_decay] * len(self.params)
+        if len(self.weight_decay) != len(self.params):
+            raise ValueError("weight_decay is a number or one per parameter")
+        if not self.params:
+            raise ValueError("no parameters")
+        self.device = self.params[0].device
+        tables = set(tables)
+        if states is None:
+            states = [alloc_adamw_state(p, bits, k in tables) for k, p in enumerate(self.params)]
+        self.states, self.bits = list(states), bits
+        self.device_steps = torch.full((1,), steps, dtype=torch.int64, device=self.device) if device_step else None
+        if len(self.states) != len(self.params):
+            raise ValueError("one state per parameter is needed")
+        self._list = (AdamWTensor * len(self.params))()
+        self._seen = [None] * len(self.params)
+        for k in range(len(self.params)):
+            self._describe(k)
+
+    def _describe(self, k: int) -> None:
+        """Checks parameter k and its moments and puts them into the list."""
+        import torch
+        p, state = self.params[k], self.states[k]
+        if p.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"parameter {k} must be fp32 or bf16, got {p.dtype}")
+        shapes = {"m": p.shape, "v": p.shape}
+        by_rows, whole = True, True
+        if self.bits == 8:
+            blocks = lambda n: -(-n // ADAMW_BLOCK)
+            whole_shape = (blocks(p.numel()),)
+            rows_shape = (p.shape[0], blocks(p.shape[1])) if p.dim() == 2 else None
+            got = tuple(state["m_scale"].shape)
+            by_rows, whole = got == rows_shape, got == whole_shape
+            if not by_rows and not whole:
+                raise ValueError(f"m_scale of parameter {k} must have shape {whole_shape}"
+                                 + (f" or {rows_shape}" if rows_shape else "") + f", got {got}")
+            shapes.update(m_scale=got, v_scale=got)
+        elif self.bits != 32:
+            raise ValueError(f"moments have 8 or 32 bits, not {self.bits}")
+        code = torch.float32 if self.bits == 32 else torch.float8_e4m3fn
+        for name, t, dtype in [("parameter", p, p.dtype)] + \
+                [(n, state[n], code if n in ("m", "v") else torch.float32) for n in shapes]:
+            numel = p.numel() if name in ("parameter", "m", "v") else None
+            if t.device != self.device or not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or \
+                    (numel is not None and t.numel() != numel) or (numel is None and tuple(t.shape) != tuple(shapes[name])):
+                raise ValueError(f"{name} of parameter {k} must be a contiguous {dtype} tensor on {self.device} that "
+                                 f"fits {tuple(p.shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        x = self._list[k]
+        x.param, x.m, x.v = p.data_ptr(), state["m"].data_ptr(), state["v"].data_ptr()
+        x.m_scale, x.v_scale = (state["m_scale"].data_ptr(), state["v_scale"].data_ptr()) if self.bits == 8 else (None, None)
+        x.n_rows, x.dim = (p.shape[0], p.shape[1]) if p.dim() == 2 else (1, p.numel())
+        x.param_type, x.bits, x.index, x.weight_decay = _types()[p.dtype], self.bits, k, self.weight_decay[k]
+        self._seen[k] = (tuple(t.data_ptr() for t in (p, *(state[n] for n in shapes))), p.shape, by_rows, whole)
+
+    def step(self, grads, grad_scale=None, stream=None) -> None:
+        """One step.  grads: for each parameter a contiguous tensor of its
+        shape (fp32, bf16 or fp16), a RowGrad for a table, or None to leave
+        it.  grad_scale: an fp32 device tensor [1] that multiplies every
+        gradient (of a norm's clipping, of a scaled loss); nothing is written
+        where it is not finite, though the step counts."""
+        import torch
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        types, used = _types(), []
+        for k, (p, g) in enumerate(zip(self.params, grads)):
+            if g is None:
+                continue
+            if p.numel() == 0:
+                continue
+            state = self.states[k]
+            seen = self._seen[k]
+            if seen[0][:3] != (p.data_ptr(), state["m"].data_ptr(), state["v"].data_ptr()) or seen[1] != p.shape:
+                self._describe(k)
+                seen = self._seen[k]
+            x = self._list[k]
+            if isinstance(g, RowGrad):
+                self._rows(k, x, p, g, seen[2], types)
+            else:
+                if g.dtype not in types or g.shape != p.shape or g.device != self.device or not g.is_contiguous():
+                    raise ValueError(f"gradient {k} must be a contiguous tensor of shape {tuple(p.shape)} on {self.device}, "
+                                     f"got {g.dtype} {tuple(g.shape)} on {g.device}")
+                if not seen[3]:
+                    raise ValueError(f"the moments of parameter {k} have scales per row: its gradient must be a RowGrad")
+                x.grad, x.grad_type, x.rows, x.order, x.coef = g.data_ptr(), types[g.dtype], None, None, None
+            used.append(k)
+        for name, t, dtype in (("lr", self.lr if isinstance(self.lr, torch.Tensor) else None, torch.float32),
+                               ("grad_scale", grad_scale, torch.float32)):
+            if t is not None and (t.dtype != dtype or t.numel() != 1 or t.device != self.device):
+                raise ValueError(f"{name} must be one {dtype} number on {self.device}")
+        if len(used) == len(self.params):
+            ts = self._list
+        else:
+            ts = (AdamWTensor * max(1, len(used)))(*[self._list[k] for k in used])
+        device_lr = isinstance(self.lr, torch.Tensor)
+        args = AdamWArgs(0.0 if device_lr else self.lr, self.betas[0], self.betas[1], self.eps, self.steps + 1,
+                         _ptr(self.device_steps), self.lr.data_ptr() if device_lr else None, _ptr(grad_scale),
+                         0 if self.seed is None else self.seed, 0 if self.seed is None else ADAMW_STOCHASTIC)
+        need = ctypes.c_size_t()
+        _check(lib().smore_adamw_workspace_bytes(ts, len(used), ctypes.byref(need)))
+        with _Launch(self.device, stream) as st:
+            ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+            if self.device_steps is not None:
+                self.device_steps.add_(1)
+            rc = lib().smore_adamw(ts, len(used), ctypes.byref(args), _ptr(ws), need.value, st)
+            if rc and self.device_steps is not None:
+                self.device_steps.sub_(1)
+            _check(rc)
+        self.steps += 1
+        # autograd sees that they changed
+        torch.autograd.graph.increment_version([self.params[k] for k in used if not self.params[k].is_inference()])
+
+    def _rows(self, k: int, x, p, g: RowGrad, by_rows: bool, types: dict) -> None:
+        import torch
+        if p.dim() != 2 or not by_rows:
+            raise ValueError(f"parameter {k} is no table with moments per row: its gradient cannot be a RowGrad")
+        n = g.rows.numel()
+        ok = lambda t, dtype, numel: t.dtype == dtype and t.device == self.device and t.is_contiguous() and t.numel() == numel
+        if not ok(g.rows, torch.int32, n):
+            raise ValueError(f"rows of gradient {k} must be a contiguous int32 tensor on {self.device}")
+        if g.order is not None and not ok(g.order, torch.int64, n):
+            raise ValueError(f"order of gradient {k} must be a contiguous int64 tensor of {n} entries on {self.device}")
+        if g.coef is not None and not ok(g.coef, torch.float32, n):
+            raise ValueError(f"coef of gradient {k} must be a contiguous fp32 tensor of {n} entries on {self.device}")
+        if g.per < 1 or g.grad.dim() != 2 or g.grad.shape[1] != p.shape[1] or g.grad.shape[0] * g.per < n or \
+                g.grad.dtype not in types or g.grad.device != self.device or not g.grad.is_contiguous():
+            raise ValueError(f"gradient {k} must hold contiguous rows of {p.shape[1]} on {self.device}, one for each "
+                             f"{g.per} of {n} entries, got {g.grad.dtype} {tuple(g.grad.shape)} on {g.grad.device}")
+        x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), types[g.grad.dtype], g.rows.data_ptr(), \
+            None if g.order is None else g.order.data_ptr(), None if g.coef is None else g.coef.data_ptr()
+        x.n_entries, x.per = n, g.per

@@ -1,13 +1,18 @@
 // capi.cpp -- host side of the C ABI declared in include/smore.h: argument
 // validation, the fourteen plan presets, the node-cut planner, compilation of a
-// plan into the positive-sampling program, and graph handle management.
-// Device work is in graph_build.hip and sample.hip.
+// plan into the positive-sampling program, and graph handle management; and
+// the checks of the training calls.  Device work is in graph_build.hip and
+// sample.hip, and in score.hip, loss.hip and adamw.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <memory>
+#include <new>
 #include <string>
 
 #include "smore_internal.h"
@@ -669,6 +674,191 @@ int smore_sample_negatives_part(const smore_graph* g, const smore_query_dag* dag
 {
     if (part < 0 || part > 2) return fail(SMORE_E_INVALID_ARG, "part must be 0, 1 or 2");
     return run_sample(g, dag, a, out, stats, workspace, ws_bytes, hip_stream, NEG, 1 << part);
+}
+
+}  // extern "C"
+
+// ------------------------------------------------- training on sampled batches
+namespace {
+
+int check_score(const smore_score_args* a)
+{
+    if (!a) return fail(SMORE_E_INVALID_ARG, "args is NULL");
+    if (a->batch < 1) return fail(SMORE_E_INVALID_ARG, "batch must be >= 1");
+    if (a->n < 0) return fail(SMORE_E_INVALID_ARG, "n must be >= 0");
+    if (a->dim < 1 || a->dim > (1 << 20)) return fail(SMORE_E_INVALID_ARG, "dim must be in [1, 2^20]");
+    if (a->n_rows < 1) return fail(SMORE_E_INVALID_ARG, "n_rows must be >= 1");
+    if (a->table_stride < a->dim || a->query_stride < a->dim || a->candidate_stride < 0 ||
+        a->score_stride < a->n)
+        return fail(SMORE_E_INVALID_ARG, "a stride is shorter than its row");
+    for (int32_t t : {a->table_type, a->query_type})
+        if (t != SMORE_F32 && t != SMORE_BF16)
+            return fail(SMORE_E_UNSUPPORTED, "tables and queries are fp32 or bf16, not type %d", t);
+    return SMORE_OK;
+}
+
+int check_preference(const smore_preference_args* a, const smore_preference_in* in,
+                     const smore_preference_out* out)
+{
+    if (!a || !in || !out) return fail(SMORE_E_INVALID_ARG, "args, in or out is NULL");
+    if (a->batch < 1) return fail(SMORE_E_INVALID_ARG, "batch must be >= 1");
+    if (a->n < 0 || a->n > (1 << 30)) return fail(SMORE_E_INVALID_ARG, "n must be in [0, 2^30]");
+    if (a->batch >= (1 << 24)) return fail(SMORE_E_OVERFLOW, "batch must stay below 2^24");
+    if (a->kind != SMORE_PREFERENCE_PAIRS && a->kind != SMORE_PREFERENCE_SOFTMAX)
+        return fail(SMORE_E_INVALID_ARG, "unknown kind %d", a->kind);
+    if (a->score_type < SMORE_F32 || a->score_type > SMORE_F16)
+        return fail(SMORE_E_UNSUPPORTED, "scores are fp32, bf16 or fp16, not type %d", a->score_type);
+    if (!(a->beta > 0.0f) || !std::isfinite(a->beta)) return fail(SMORE_E_INVALID_ARG, "beta must be finite and > 0");
+    if (!(a->smoothing >= 0.0f && a->smoothing < 1.0f))
+        return fail(SMORE_E_INVALID_ARG, "smoothing must be in [0, 1)");
+    if (a->kind == SMORE_PREFERENCE_SOFTMAX && a->smoothing != 0.0f)
+        return fail(SMORE_E_INVALID_ARG, "smoothing is for pairs");
+    if (!std::isfinite(a->scale)) return fail(SMORE_E_INVALID_ARG, "scale must be finite");
+    if (!in->positive || (a->n > 0 && !in->negatives)) return fail(SMORE_E_INVALID_ARG, "scores are NULL");
+    if (a->n > 0 && !in->ref_positive != !in->ref_negatives)
+        return fail(SMORE_E_INVALID_ARG, "reference scores are given for both, or for neither");
+    if (in->n_valid && in->mask) return fail(SMORE_E_INVALID_ARG, "n_valid or mask, not both");
+    if (a->n > 0 && !out->grad_positive != !out->grad_negatives)
+        return fail(SMORE_E_INVALID_ARG, "gradients are wanted for both, or for neither");
+    if (!out->loss && !out->grad_positive) return fail(SMORE_E_INVALID_ARG, "no output is wanted");
+    if (a->positive_stride < 0 || a->negatives_stride < 0 || a->ref_positive_stride < 0 || a->ref_negatives_stride < 0)
+        return fail(SMORE_E_INVALID_ARG, "a stride is negative");
+    if (a->batch > 1 && out->grad_positive && (a->grad_positive_stride < 1 || a->grad_negatives_stride < a->n))
+        return fail(SMORE_E_INVALID_ARG, "rows of a gradient overlap");
+    return SMORE_OK;
+}
+
+int check_adamw_tensor(const smore_adamw_tensor& t, int k)
+{
+    if (!t.param || !t.m || !t.v) return fail(SMORE_E_INVALID_ARG, "tensor %d: a pointer is NULL", k);
+    if (t.param_type != SMORE_F32 && t.param_type != SMORE_BF16)
+        return fail(SMORE_E_UNSUPPORTED, "tensor %d: parameters are fp32 or bf16, not type %d", k, t.param_type);
+    if (t.grad_type < SMORE_F32 || t.grad_type > SMORE_F16)
+        return fail(SMORE_E_UNSUPPORTED, "tensor %d: gradients are fp32, bf16 or fp16, not type %d", k, t.grad_type);
+    if (t.bits != 8 && t.bits != 32)
+        return fail(SMORE_E_UNSUPPORTED, "tensor %d: moments have 8 or 32 bits, not %d", k, t.bits);
+    if (t.bits == 8 && (!t.m_scale || !t.v_scale))
+        return fail(SMORE_E_INVALID_ARG, "tensor %d: moments in 8 bits need their scales", k);
+    if (t.n_rows < 1 || t.dim < 1) return fail(SMORE_E_INVALID_ARG, "tensor %d: n_rows and dim must be >= 1", k);
+    if (!std::isfinite(t.weight_decay)) return fail(SMORE_E_INVALID_ARG, "tensor %d: weight_decay must be finite", k);
+    if (t.n_rows > INT64_MAX / t.dim) return fail(SMORE_E_OVERFLOW, "tensor %d: too many elements", k);
+    if (!t.rows) {
+        if (!t.grad) return fail(SMORE_E_INVALID_ARG, "tensor %d: grad is NULL", k);
+        if (t.n_rows * t.dim >= (int64_t)1 << 34)
+            return fail(SMORE_E_OVERFLOW, "tensor %d: elements must stay below 2^34", k);
+        return SMORE_OK;
+    }
+    if (t.n_rows > INT32_MAX) return fail(SMORE_E_OVERFLOW, "tensor %d: n_rows must be an int32", k);
+    if (t.n_entries < 0) return fail(SMORE_E_INVALID_ARG, "tensor %d: n_entries must be >= 0", k);
+    if (t.n_entries >= (int64_t)1 << 26) return fail(SMORE_E_OVERFLOW, "tensor %d: entries must stay below 2^26", k);
+    if (t.n_entries > 0 && !t.grad) return fail(SMORE_E_INVALID_ARG, "tensor %d: grad is NULL", k);
+    if (t.per < 1) return fail(SMORE_E_INVALID_ARG, "tensor %d: per must be >= 1", k);
+    return SMORE_OK;
+}
+
+// No two tensors step the same memory.
+int check_adamw_overlap(const smore_adamw_tensor* ts, int n)
+{
+    struct Span {
+        uintptr_t first, end;
+        int k;
+    };
+    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[n]);
+    if (!spans) return fail(SMORE_E_NOMEM, "host allocation failed");
+    for (int k = 0; k < n; ++k) {
+        const uintptr_t at = (uintptr_t)ts[k].param;
+        spans[k] = {at, at + (uintptr_t)(ts[k].n_rows * ts[k].dim) * (ts[k].param_type == SMORE_BF16 ? 2 : 4), k};
+    }
+    std::sort(spans.get(), spans.get() + n, [](const Span& a, const Span& b) { return a.first < b.first; });
+    for (int k = 1; k < n; ++k)
+        if (spans[k].first < spans[k - 1].end)
+            return fail(SMORE_E_INVALID_ARG, "parameters of tensors %d and %d overlap", spans[k - 1].k, spans[k].k);
+    return SMORE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int smore_score(const smore_score_args* a, const void* table, const void* queries, const int32_t* candidates,
+                float* scores, void* hip_stream)
+{
+    int rc = check_score(a);
+    if (rc) return rc;
+    if (a->n == 0) return ok();
+    if (!table || !queries || !candidates || !scores) return fail(SMORE_E_INVALID_ARG, "a buffer is NULL");
+    // wavefronts of the finest division, and the threads of a grid's 2^32
+    if ((int64_t)a->batch * ((a->n + 7) / 8) >= (int64_t)1 << 26)
+        return fail(SMORE_E_OVERFLOW, "batch x ceil(n / 8) must stay below 2^26");
+    const char* err = "";
+    rc = smore::launch_score(*a, table, queries, candidates, scores, (hipStream_t)hip_stream, &err);
+    return rc ? fail(rc, "smore_score: %s", err) : ok();
+}
+
+int smore_score_grad_workspace_bytes(const smore_score_args* a, size_t* bytes)
+{
+    if (!bytes) return fail(SMORE_E_INVALID_ARG, "bytes is NULL");
+    const int rc = check_score(a);
+    if (rc) return rc;
+    *bytes = smore::score_grad_workspace(*a);
+    return ok();
+}
+
+int smore_score_grad(const smore_score_args* a, const void* table, const int32_t* candidates, const float* grad_scores,
+                     void* grad_queries, void* workspace, size_t ws_bytes, void* hip_stream)
+{
+    int rc = check_score(a);
+    if (rc) return rc;
+    if (!grad_queries || (a->n > 0 && (!table || !candidates || !grad_scores)))
+        return fail(SMORE_E_INVALID_ARG, "a buffer is NULL");
+    if (a->batch >= (1 << 24)) return fail(SMORE_E_OVERFLOW, "batch must stay below 2^24");
+    const size_t need = smore::score_grad_workspace(*a);
+    if (need && (!workspace || ws_bytes < need))
+        return fail(SMORE_E_INVALID_ARG, "workspace missing or smaller than %zu bytes", need);
+    const char* err = "";
+    rc = smore::launch_score_grad(*a, table, candidates, grad_scores, grad_queries, workspace, (hipStream_t)hip_stream, &err);
+    return rc ? fail(rc, "smore_score_grad: %s", err) : ok();
+}
+
+int smore_preference_loss(const smore_preference_args* a, const smore_preference_in* in, const smore_preference_out* out,
+                          void* hip_stream)
+{
+    int rc = check_preference(a, in, out);
+    if (rc) return rc;
+    const char* err = "";
+    rc = smore::launch_preference(*a, *in, *out, (hipStream_t)hip_stream, &err);
+    return rc ? fail(rc, "smore_preference_loss: %s", err) : ok();
+}
+
+int smore_adamw_workspace_bytes(const smore_adamw_tensor* ts, int32_t n, size_t* bytes)
+{
+    if (!ts || !bytes || n < 0) return fail(SMORE_E_INVALID_ARG, "NULL argument or n_tensors < 0");
+    for (int k = 0; k < n; ++k)
+        if (int rc = check_adamw_tensor(ts[k], k)) return rc;
+    *bytes = smore::adamw_workspace(ts, n);
+    return ok();
+}
+
+int smore_adamw(const smore_adamw_tensor* ts, int32_t n, const smore_adamw_args* a, void* workspace, size_t ws_bytes,
+                void* hip_stream)
+{
+    if (!a || n < 0 || (n > 0 && !ts)) return fail(SMORE_E_INVALID_ARG, "NULL argument or n_tensors < 0");
+    if (!(a->lr >= 0.0) || !std::isfinite(a->lr)) return fail(SMORE_E_INVALID_ARG, "lr must be finite and >= 0");
+    if (!(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0))
+        return fail(SMORE_E_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
+    if (!(a->eps >= 0.0) || !std::isfinite(a->eps)) return fail(SMORE_E_INVALID_ARG, "eps must be finite and >= 0");
+    if (a->step < 1) return fail(SMORE_E_INVALID_ARG, "step must be >= 1");
+    if (a->flags & ~SMORE_ADAMW_STOCHASTIC) return fail(SMORE_E_INVALID_ARG, "unknown flags 0x%x", a->flags);
+    int rc;
+    for (int k = 0; k < n; ++k)
+        if ((rc = check_adamw_tensor(ts[k], k))) return rc;
+    if ((rc = check_adamw_overlap(ts, n))) return rc;
+    const size_t need = smore::adamw_workspace(ts, n);
+    if (need && (!workspace || ws_bytes < need))
+        return fail(SMORE_E_INVALID_ARG, "workspace missing or smaller than %zu bytes", need);
+    const char* err = "";
+    rc = smore::launch_adamw(ts, n, *a, workspace, (hipStream_t)hip_stream, &err);
+    return rc ? fail(rc, "smore_adamw: %s", err) : ok();
 }
 
 }  // extern "C"
