@@ -32,21 +32,27 @@ namespace {
 
 constexpr int WG = 256;
 constexpr int WAVES = WG / 64;
-constexpr int PER = 4;                  // consecutive elements of a lane
-constexpr int CHUNK = 64 * PER;         // elements of a wavefront: two blocks of 128
+constexpr int PER = 8;                  // consecutive elements of a lane
+constexpr int CHUNK = 64 * PER;         // elements of a wavefront: four blocks of 128
 constexpr int BLOCK = SMORE_ADAMW_BLOCK;
-constexpr int CHUNKS = 4;               // chunks of a wavefront in a dense tensor
 constexpr int RUN = 128;                // entries whose sum is made ahead in long runs
 
+// One step's constants.
+struct Step {
+    float rate, keep, b1, b2, a1, a2, eps;   // a = 1 - b
+    float move, root;                        // rate / (1 - b1^t), 1 / sqrt(1 - b2^t)
+    float scale;                             // of the gradients
+    uint32_t key;
+};
+
 struct Hyper {
-    float lr, b1, b2, eps, c1, c2;      // c1 = 1 - b1^t, c2 = 1 - b2^t where the step is given
+    Step s;                             // as the host knows it (keep and move for decay 0)
     float log_b1, log_b2;
     const int64_t* step;                // step, rate and gradient scale on the device, or NULL
     const float* lr_dev;
     const float* grad_scale;
-    int64_t step_host;
-    uint64_t seed;
-    int32_t stochastic;
+    uint32_t seed_key;
+    int32_t stochastic, on_device;
 };
 
 struct Tensor {
@@ -72,11 +78,13 @@ struct RowsTensor {
     const int32_t* rows;
     const int64_t* order;
     const float* coef;
-    const float* partial;
-    int64_t n_rows, dim, n_entries, per;
+    const double* partial;
+    double per_inverse;
+    int64_t n_rows, dim, n_entries;
+    uint32_t per;
 };
 
-__device__ __forceinline__ uint32_t mix(uint32_t x)
+__host__ __device__ inline uint32_t mix(uint32_t x)
 {
     x ^= x >> 16;
     x *= 0x7FEB352Du;
@@ -84,63 +92,98 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
     x *= 0x846CA68Bu;
     return x ^ (x >> 16);
 }
+// Key of a step's roundings; a tensor's is mix(key + index).
+__host__ __device__ inline uint32_t step_key(uint32_t seed_key, int64_t t)
+{
+    return mix(mix(seed_key + (uint32_t)t) ^ (uint32_t)((uint64_t)t >> 32));
+}
 
-// One step's constants and the key of one tensor's roundings.
-struct Step {
-    float rate, keep, b1, b2, eps, r1, r2, scale;   // r1 = 1 / c1, r2 = 1 / c2
-    uint32_t key;
-    bool stochastic, skip;
-    __device__ Step(const Hyper& h, float decay, int32_t index)
-    {
-        const int64_t t = h.step ? *h.step : h.step_host;
-        const float c1 = h.step ? -expm1f((float)t * h.log_b1) : h.c1;
-        const float c2 = h.step ? -expm1f((float)t * h.log_b2) : h.c2;
-        rate = h.lr_dev ? *h.lr_dev : h.lr;
-        keep = 1.0f - rate * decay;
-        b1 = h.b1;
-        b2 = h.b2;
-        eps = h.eps;
-        r1 = 1.0f / c1;
-        r2 = 1.0f / c2;
-        scale = h.grad_scale ? *h.grad_scale : 1.0f;
-        skip = !(fabsf(scale) < INFINITY);
-        stochastic = h.stochastic != 0;
-        uint32_t k = mix(mix((uint32_t)h.seed) ^ (uint32_t)(h.seed >> 32));
-        k = mix(mix(k + (uint32_t)t) ^ (uint32_t)((uint64_t)t >> 32));
-        key = mix(k + (uint32_t)index);
+// The step's constants for one tensor; false where nothing is to be written.
+__device__ __forceinline__ bool step_of(const Hyper& h, const Tensor& t, Step* s)
+{
+    *s = h.s;
+    if (h.on_device) {
+        if (h.lr_dev) {
+            s->move *= *h.lr_dev;       // the host's is of rate 1
+            s->rate = *h.lr_dev;
+        }
+        if (h.step) {
+            const int64_t at = *h.step;
+            s->move = s->rate / -expm1f((float)at * h.log_b1);
+            s->root = 1.0f / sqrtf(-expm1f((float)at * h.log_b2));
+            s->key = step_key(h.seed_key, at);
+        }
+        if (h.grad_scale) s->scale = *h.grad_scale;
+        if (!(fabsf(s->scale) < INFINITY)) return false;
     }
-};
+    s->keep = 1.0f - s->rate * t.decay;
+    s->key = mix(s->key + (uint32_t)t.index);
+    return true;
+}
 
-// Codes: e4m3 (4 exponent bits, 3 fraction bits, no infinity), y in [0, 448].
-// A value's bits above the fraction's are its code, once the exponent's bias
-// is moved from 127 to 7; below 2^-6 codes are multiples of 2^-9.
-__device__ __forceinline__ uint32_t encode(float y, uint32_t draw, bool stochastic)
+// Square root to the nearest (but for 1 in 10^7, which the tie-breaking bits
+// are not fine enough to see): one Newton step from the estimate's residual.
+// The moments take the same roundings as IEEE arithmetic, so that their codes
+// do not depend on how a product and a sum are fused.
+__device__ __forceinline__ float root_of(float v)
+{
+    const float r = __builtin_amdgcn_rsqf(fmaxf(v, 1.17549435e-38f));
+    const float s = v * r;
+    return fmaf(fmaf(-s, s, v), 0.5f * r, s);
+}
+
+__device__ __forceinline__ float first_moment(float m, float g, const Step& s)
+{
+#pragma clang fp contract(off)
+    const float kept = s.b1 * m, added = s.a1 * g;
+    return kept + added;
+}
+__device__ __forceinline__ float second_moment(float v, float g, const Step& s)
+{
+#pragma clang fp contract(off)
+    const float square = g * g;
+    const float kept = s.b2 * v, added = s.a2 * square;
+    return kept + added;
+}
+
+// e4m3 (4 exponent bits of bias 7, 3 fraction bits, no infinity) is what is
+// left of fp32 times 2^-120 without its 20 lowest bits: the exponent's bias
+// moves from 127 to 7, and e4m3's subnormals below 2^-6 are fp32's below
+// 2^-126.  Rounding is an addition to those 20 bits, before they go; values
+// up to 448 (and a few half steps above) cannot be carried past 448.
+constexpr float TO_CODE = 0x1p-120f;
+constexpr float LEAST_CODE = 0x1p-129f;
+
+// Bits of a value (relative to its block's largest, times 448) whose bits 20
+// to 26, and 31, are its code.
+__device__ __forceinline__ uint32_t code_bits(float y, uint32_t draw, bool stochastic)
 {
     const uint32_t bits = __float_as_uint(y);
-    const float fine = y * 512.0f;
-    uint32_t up, small;
-    if (stochastic) {
-        up = draw << 4;
-        const float whole = floorf(fine);
-        small = (uint32_t)whole + ((fine - whole) * 65536.0f + (float)draw >= 65536.0f ? 1u : 0u);
-    } else {
-        up = 0x7FFFFu + ((bits >> 20) & 1u);
-        small = (uint32_t)rintf(fine);
-    }
-    const uint32_t code = y < 0.015625f ? small : ((bits + up) >> 20) - (120u << 3);
-    return code < 0x7Eu ? code : 0x7Eu;
+    return stochastic ? bits + (draw << 4) : bits + 0x7FFFFu + ((bits >> 20) & 1u);
+}
+// Four codes of such bits: sign and magnitude moved to the top byte each,
+// then the top bytes gathered.
+__device__ __forceinline__ uint32_t gather_codes(const uint32_t* bits)
+{
+    uint32_t x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = ((bits[j] << 4) & 0x7FFFFFFFu) | (bits[j] & 0x80000000u);
+    const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x0C0C0703u);   // bytes 3 of x[0] and x[1]
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(x[3], x[2], 0x07030C0Cu), lo, 0x07060100u);
 }
 
 // Values of four codes.
 __device__ __forceinline__ void decode(uint32_t four, float* out)
 {
-    out[0] = __builtin_amdgcn_cvt_f32_fp8((int)four, 0);
-    out[1] = __builtin_amdgcn_cvt_f32_fp8((int)four, 1);
-    out[2] = __builtin_amdgcn_cvt_f32_fp8((int)four, 2);
-    out[3] = __builtin_amdgcn_cvt_f32_fp8((int)four, 3);
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)four, false);
+    const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)four, true);
+    out[0] = a[0];
+    out[1] = a[1];
+    out[2] = b[0];
+    out[3] = b[1];
 }
 
-// Largest magnitude of the 32 lanes of a block, as bits: NaN above infinity
+// Largest magnitude of the 16 lanes of a block, as bits: NaN above infinity
 // above every number.
 __device__ __forceinline__ uint32_t block_max(uint32_t x)
 {
@@ -150,36 +193,34 @@ __device__ __forceinline__ uint32_t block_max(uint32_t x)
     SMORE_STEP(DPP_MIRROR8);
     SMORE_STEP(DPP_MIRROR16);
 #undef SMORE_STEP
-    return max(x, (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F));   // lane ^ 16
+    return x;
 }
 
 // Scale of a block and the factor that takes its values to [0, 448].
 __device__ __forceinline__ void block_scale(uint32_t top_bits, float* scale, float* unit)
 {
     const float top = __uint_as_float(top_bits);
-    if (top_bits >= 0x7F800000u) {
-        *scale = __uint_as_float(0x7FC00000u);
-        *unit = 0.0f;
-    } else if (top < 1.17549435e-38f) {
-        *scale = *unit = 0.0f;
-    } else {
-        *scale = top / 448.0f;
-        *unit = 448.0f / top;
-    }
+    const bool some = top >= 1.17549435e-38f;
+    *scale = top_bits >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : some ? top * (1.0f / 448.0f) : 0.0f;
+    *unit = some ? (1.0f / top) * 448.0f : 0.0f;
 }
 
+// Parameters of a lane, rounded; bf16 stochastically by bits that are a
+// product's of the element's draw.
 __device__ __forceinline__ float to_param(float p, uint32_t, bool, float) { return p; }
 __device__ __forceinline__ bf16 to_param(float p, uint32_t draw, bool stochastic, bf16)
 {
-    if (!stochastic || !(fabsf(p) < INFINITY)) return (bf16)p;
+    if (!stochastic) return (bf16)p;
     const uint32_t up = ((draw ^ 0x85EBCA6Bu) * 0x9E3779B1u) >> 16;
-    const uint16_t top = (uint16_t)((__float_as_uint(p) + up) >> 16);
+    const uint32_t bits = __float_as_uint(p);
+    // a NaN's lower bits could be carried into its sign
+    const uint16_t top = (uint16_t)((p == p ? bits + up : 0x7FC00000u) >> 16);
     bf16 out;
     __builtin_memcpy(&out, &top, sizeof(out));
     return out;
 }
 
-// Elements and moments of a chunk that a lane holds.
+// Elements and moments that a lane holds.
 template <int BITS>
 struct Held;
 template <>
@@ -188,57 +229,57 @@ struct Held<32> {
 };
 template <>
 struct Held<8> {
-    uint32_t m, v;
+    uint32_t m[PER / 4], v[PER / 4];
     float m_scale, v_scale;
 };
 
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t have)
+__device__ __forceinline__ void load_codes(const uint8_t* p, int64_t have, uint32_t* x)
 {
-    uint32_t x = 0;
     if (have >= PER) {
-        __builtin_memcpy(&x, p, 4);
+        __builtin_memcpy(x, p, PER);
     } else {
 #pragma unroll
+        for (int k = 0; k < PER / 4; ++k) x[k] = 0;
+#pragma unroll
         for (int j = 0; j < PER - 1; ++j)
-            if (j < have) x |= (uint32_t)p[j] << (8 * j);
+            if (j < have) x[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
     }
-    return x;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t have, uint32_t x)
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t have, const uint32_t* x)
 {
     if (have >= PER) {
-        __builtin_memcpy(p, &x, 4);
+        __builtin_memcpy(p, x, PER);
     } else {
 #pragma unroll
         for (int j = 0; j < PER - 1; ++j)
-            if (j < have) p[j] = (uint8_t)(x >> (8 * j));
+            if (j < have) p[j] = (uint8_t)(x[j / 4] >> (8 * (j % 4)));
     }
 }
 
 // at: the lane's first element in the tensor; have: how many of its PER
-// elements the row has (none: <= 0); scale_at: its block's scale.
+// elements the row has (none: <= 0); block: number of its 128-element block.
 template <int BITS>
-__device__ __forceinline__ void load_held(const Tensor& t, int64_t at, int64_t have, int64_t scale_at, Held<BITS>& h)
+__device__ __forceinline__ void load_held(const Tensor& t, int64_t at, int64_t have, int64_t block, Held<BITS>& h)
 {
     if constexpr (BITS == 32) {
         load_floats<float, PER>((const float*)t.m + at, have, h.m);
         load_floats<float, PER>((const float*)t.v + at, have, h.v);
     } else {
-        h.m = load_codes((const uint8_t*)t.m + at, have);
-        h.v = load_codes((const uint8_t*)t.v + at, have);
-        h.m_scale = have > 0 ? t.m_scale[scale_at] : 0.0f;
-        h.v_scale = have > 0 ? t.v_scale[scale_at] : 0.0f;
+        load_codes((const uint8_t*)t.m + at, have, h.m);
+        load_codes((const uint8_t*)t.v + at, have, h.v);
+        h.m_scale = have > 0 ? t.m_scale[block] : 0.0f;
+        h.v_scale = have > 0 ? t.v_scale[block] : 0.0f;
     }
 }
 
 // Steps a lane's PER elements and writes them back.  Every lane of the
-// wavefront takes part (the maxima of the 8-bit blocks).  block: number of
-// the 128-element block; j0: the lane's first element in it.
+// wavefront takes part (the maxima of the 8-bit blocks).  j0: the lane's
+// first element in its block.
 template <class TP, int BITS>
-__device__ __forceinline__ void step_held(const Tensor& t, const Step& s, int64_t at, int64_t have, int64_t block, int j0,
-                                          float* p, const float* g, Held<BITS>& h)
+__device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool stochastic, int64_t at, int64_t have,
+                                          int64_t block, int j0, float* p, const float* g, Held<BITS>& h)
 {
-    float m[PER], v[PER];
+    float m[PER], v[PER], u[PER];
     if constexpr (BITS == 32) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
@@ -246,8 +287,11 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, int64_
             v[j] = h.v[j];
         }
     } else {
-        decode(h.m, m);
-        decode(h.v, v);
+#pragma unroll
+        for (int k = 0; k < PER / 4; ++k) {
+            decode(h.m[k], m + 4 * k);
+            decode(h.v[k], v + 4 * k);
+        }
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             m[j] *= h.m_scale;
@@ -258,21 +302,22 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, int64_
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const float gj = g[j] * s.scale;
-        m[j] = s.b1 * m[j] + (1.0f - s.b1) * gj;
-        v[j] = s.b2 * v[j] + (1.0f - s.b2) * (gj * gj);
-        p[j] = p[j] * s.keep - s.rate * ((m[j] * s.r1) / (sqrtf(v[j] * s.r2) + s.eps));
+        m[j] = first_moment(m[j], gj, s);
+        v[j] = second_moment(v[j], gj, s);
+        u[j] = BITS == 8 ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
+        p[j] = fmaf(-s.move * m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.root, s.eps)), p[j] * s.keep);
     }
     constexpr bool DRAWS = BITS == 8 || sizeof(TP) == 2;
     uint32_t draw[PER] = {};
-    if (DRAWS && s.stochastic) {
-        const uint32_t base = mix(mix(s.key ^ (uint32_t)block) + (uint32_t)((uint64_t)block >> 32));
+    if (DRAWS && stochastic) {
+        const uint32_t base = mix(mix(s.key ^ (uint32_t)block) + (uint32_t)((uint64_t)block >> 32)) + (uint32_t)j0;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) draw[j] = mix(base + (uint32_t)(j0 + j));
+        for (int j = 0; j < PER; ++j) draw[j] = mix(base + (uint32_t)j);
     }
     if (have > 0) {
         Vec<TP, PER> out;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) out.x[j] = to_param(p[j], draw[j], s.stochastic, TP{});
+        for (int j = 0; j < PER; ++j) out.x[j] = to_param(p[j], draw[j], stochastic, TP{});
         TP* dst = (TP*)t.p + at;
         if (have >= PER) {
             store_vec<TP, PER>(dst, out);
@@ -288,32 +333,40 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, int64_
             store_floats<float, PER>((float*)t.v + at, have, v);
         }
     } else {
-        uint32_t m_top = 0, v_top = 0;
+        uint32_t m_top = 0, u_top = 0;
+        if (have < PER) {
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            if (j >= have) m[j] = v[j] = 0.0f;
-            v[j] = sqrtf(v[j]);
-            m_top = max(m_top, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-            v_top = max(v_top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+            for (int j = 0; j < PER; ++j)
+                if (j >= have) m[j] = u[j] = 0.0f;
         }
-        float m_scale, m_unit, v_scale, v_unit;
-        block_scale(block_max(m_top), &m_scale, &m_unit);
-        block_scale(block_max(v_top), &v_scale, &v_unit);
-        uint32_t mc = 0, vc = 0;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            const uint32_t a = encode(fabsf(m[j]) * m_unit, draw[j] & 0xFFFFu, s.stochastic);
-            uint32_t b = encode(v[j] * v_unit, draw[j] >> 16, s.stochastic);
-            if (v[j] != 0.0f && v_unit > 0.0f) b = max(b, 1u);
-            mc |= (a | (m[j] < 0.0f ? 0x80u : 0u)) << (8 * j);
-            vc |= b << (8 * j);
+            m_top = max(m_top, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+            u_top = max(u_top, __float_as_uint(u[j]) & 0x7FFFFFFFu);
+        }
+        float m_scale, m_unit, u_scale, u_unit;
+        block_scale(block_max(m_top), &m_scale, &m_unit);
+        block_scale(block_max(u_top), &u_scale, &u_unit);
+        uint32_t mc[PER], uc[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            mc[j] = code_bits((m[j] * m_unit) * TO_CODE, draw[j] & 0xFFFFu, stochastic);
+            // a root that is not 0 has a code that is not 0
+            const uint32_t low = u[j] != 0.0f && u_unit > 0.0f ? __float_as_uint(LEAST_CODE) : 0u;
+            uc[j] = max(code_bits((u[j] * u_unit) * TO_CODE, draw[j] >> 16, stochastic), low);
         }
         if (have > 0) {
-            store_codes((uint8_t*)t.m + at, have, mc);
-            store_codes((uint8_t*)t.v + at, have, vc);
+            uint32_t m4[PER / 4], u4[PER / 4];
+#pragma unroll
+            for (int k = 0; k < PER / 4; ++k) {
+                m4[k] = gather_codes(mc + 4 * k);
+                u4[k] = gather_codes(uc + 4 * k);
+            }
+            store_codes((uint8_t*)t.m + at, have, m4);
+            store_codes((uint8_t*)t.v + at, have, u4);
             if (j0 == 0) {
                 t.m_scale[block] = m_scale;
-                t.v_scale[block] = v_scale;
+                t.v_scale[block] = u_scale;
             }
         }
     }
@@ -321,7 +374,7 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, int64_
 
 // A workgroup takes WAVES x CHUNKS chunks of one tensor; which one it finds
 // among the launch's tensors by their first workgroups.
-template <class TP, class TG, int BITS>
+template <class TP, class TG, int BITS, int CHUNKS>
 __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper hyper)
 {
     int lo = 0, hi = list.n - 1;
@@ -331,8 +384,9 @@ __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper
         else hi = mid - 1;
     }
     const Tensor& t = list.t[lo];
-    const Step s(hyper, t.decay, t.index);
-    if (s.skip) return;
+    Step s;
+    if (!step_of(hyper, t, &s)) return;
+    const bool stochastic = hyper.stochastic;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t base = ((int64_t)(blockIdx.x - t.first_wg) * WAVES + wave) * (CHUNK * CHUNKS) + lane * PER;
     float p[CHUNKS][PER], g[CHUNKS][PER];
@@ -347,36 +401,49 @@ __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int64_t at = base + c * CHUNK;
-        step_held<TP, BITS>(t, s, at, t.count - at, at / BLOCK, (int)(at % BLOCK), p[c], g[c], h[c]);
+        step_held<TP, BITS>(t, s, stochastic, at, t.count - at, at / BLOCK, (int)(at % BLOCK), p[c], g[c], h[c]);
     }
 }
 
-// Gradient of a table row: the entries of the sorted list that name it, each
-// coef[order[i]] times the vector order[i] / per.
+// Entries of the sorted list that name a row: coefficient and source vector
+// of entry at + lane.
+struct Entry {
+    float w;
+    uint32_t from;
+};
+__device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64_t end)
+{
+    Entry e{0.0f, 0u};
+    if (at < end) {
+        const int64_t o = r.order ? r.order[at] : at;
+        if (o >= 0 && o < r.n_entries) {   // a permutation's: reads nothing behind the gradients otherwise
+            e.w = r.coef ? r.coef[o] : 1.0f;
+            uint32_t q = (uint32_t)((double)o * r.per_inverse);   // off by one at most
+            if ((uint64_t)q * r.per > (uint64_t)o) --q;
+            if ((uint64_t)(q + 1) * r.per <= (uint64_t)o) ++q;
+            e.from = q;
+        }
+    }
+    return e;
+}
+
+// Adds the entries [first, end): products in fp32, their sum in 64 bits, so
+// that long runs lose nothing and the order does not show.
 template <class TG>
 __device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, int64_t end, int64_t col, int64_t have,
-                                            float* g)
+                                            double* g)
 {
     const int lane = threadIdx.x & 63;
     for (int64_t at = first; at < end; at += 64) {
         const int n = (int)min((int64_t)64, end - at);
-        int64_t from = 0;
-        float w = 0.0f;
-        if (lane < n) {
-            const int64_t o = r.order ? r.order[at + lane] : at + lane;
-            if (o >= 0 && o < r.n_entries) {   // a permutation's: reads nothing behind the gradients otherwise
-                w = r.coef ? r.coef[o] : 1.0f;
-                from = r.per == 1 ? o : o / r.per;
-            }
-        }
+        const Entry e = entry_of(r, at + lane, end);
         for (int i = 0; i < n; ++i) {
-            const int64_t src = ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(from >> 32), i) << 32) |
-                                (uint32_t)__builtin_amdgcn_readlane((int)from, i);
-            const float wi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i));
+            const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, i);
+            const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i));
             float x[PER];
             load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x);
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] = fmaf(wi, x[j], g[j]);
+            for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[j]);
         }
     }
 }
@@ -384,7 +451,7 @@ __device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, 
 // Sums of RUN consecutive entries of one row, where a run is that long, so
 // that no wavefront has to add a hub's entries one by one.
 template <class TG>
-__global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, float* __restrict__ partial)
+__global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, double* __restrict__ partial)
 {
     const int lane = threadIdx.x & 63;
     const int64_t c = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
@@ -393,9 +460,11 @@ __global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, float* __re
     if (row < 0 || row >= r.n_rows || r.rows[c * RUN + RUN - 1] != row) return;
     for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
         const int64_t have = r.dim - col;
-        float g[PER] = {};
+        double g[PER] = {};
         add_entries<TG>(r, c * RUN, (c + 1) * RUN, col, have, g);
-        if (have > 0) store_floats<float, PER>(partial + c * r.dim + col, have, g);
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (j < have) partial[c * r.dim + col + j] = g[j];
     }
 }
 
@@ -404,18 +473,21 @@ template <class TP, class TG, int BITS>
 __global__ __launch_bounds__(WG) void k_adamw_rows(const RowsTensor r, const Hyper hyper)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t i = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
+    const int64_t i = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * WAVES + (threadIdx.x >> 6)));
     if (i >= r.n_entries) return;
     const int32_t row = r.rows[i];
     if (row < 0 || row >= r.n_rows || (i > 0 && r.rows[i - 1] == row)) return;
-    const Step s(hyper, r.t.decay, r.t.index);
-    if (s.skip) return;
+    Step s;
+    if (!step_of(hyper, r.t, &s)) return;
+    const bool stochastic = hyper.stochastic;
+    const bool single = i + 1 >= r.n_entries || r.rows[i + 1] != row;
+    const Entry only = entry_of(r, i, i + 1);
     // [i, head): entries up to the run's end or the first sum made ahead;
     // then `sums` of those; then [tail, end)
     int64_t head = i + 1;
     int sums = 0;
     int64_t tail = 0, end = 0;
-    if (i + 1 < r.n_entries && r.rows[i + 1] == row) {
+    if (!single) {
         const int64_t next = (i + RUN - 1) / RUN * RUN;
         bool open = true;
         auto walk = [&](int64_t from, int64_t to) {   // the run's end within [from, to)
@@ -445,31 +517,39 @@ __global__ __launch_bounds__(WG) void k_adamw_rows(const RowsTensor r, const Hyp
     const int64_t blocks = (r.dim + BLOCK - 1) / BLOCK;
     for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
         const int64_t have = r.dim - col, at = (int64_t)row * r.dim + col, block = row * blocks + col / BLOCK;
-        float p[PER], g[PER] = {};
+        float p[PER], g[PER];
         Held<BITS> h;
         load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
         load_held<BITS>(r.t, at, have, block, h);
-        add_entries<TG>(r, i, head, col, have, g);
-        const float* from = r.partial + (tail / RUN - sums) * r.dim + col;
-        for (int k = 0; k < sums; ++k, from += r.dim) {
-            float x[PER];
-            load_floats<float, PER>(from, have, x);
+        if (single) {
+            load_floats<TG, PER>((const TG*)r.t.g + (int64_t)only.from * r.dim + col, have, g);
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] += x[j];
+            for (int j = 0; j < PER; ++j) g[j] *= only.w;
+        } else {
+            double sum[PER] = {};
+            add_entries<TG>(r, i, head, col, have, sum);
+            const double* from = r.partial + (tail / RUN - sums) * r.dim + col;
+            for (int k = 0; k < sums; ++k, from += r.dim) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j)
+                    if (j < have) sum[j] += from[j];
+            }
+            add_entries<TG>(r, tail, end, col, have, sum);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) g[j] = (float)sum[j];
         }
-        add_entries<TG>(r, tail, end, col, have, g);
-        step_held<TP, BITS>(r.t, s, at, have, block, (int)(col % BLOCK), p, g, h);
+        step_held<TP, BITS>(r.t, s, stochastic, at, have, block, (int)(col % BLOCK), p, g, h);
     }
 }
 
-template <class TP, class TG, int BITS>
-int dense_as(const smore_adamw_tensor* ts, int n, const Hyper& h, hipStream_t st, const char** err)
+template <class TP, class TG, int BITS, int CHUNKS>
+int dense_chunks(const smore_adamw_tensor* ts, int n, const Hyper& h, hipStream_t st, const char** err)
 {
     TensorList list;
     list.n = 0;
     uint64_t wgs = 0;
     auto flush = [&] {
-        if (list.n) k_adamw<TP, TG, BITS><<<(unsigned)wgs, WG, 0, st>>>(list, h);
+        if (list.n) k_adamw<TP, TG, BITS, CHUNKS><<<(unsigned)wgs, WG, 0, st>>>(list, h);
         list.n = 0;
         wgs = 0;
     };
@@ -487,7 +567,17 @@ int dense_as(const smore_adamw_tensor* ts, int n, const Hyper& h, hipStream_t st
 }
 
 template <class TP, class TG, int BITS>
-int rows_as(const smore_adamw_tensor& x, const Hyper& h, float* partial, hipStream_t st, const char** err)
+int dense_as(const smore_adamw_tensor* ts, int n, const Hyper& h, hipStream_t st, const char** err)
+{
+    // two chunks of a wavefront in flight, where that leaves enough wavefronts
+    int64_t total = 0;
+    for (int k = 0; k < n; ++k) total += ts[k].n_rows * ts[k].dim;
+    if (total < (int64_t)CHUNK * WAVES * 4096) return dense_chunks<TP, TG, BITS, 1>(ts, n, h, st, err);
+    return dense_chunks<TP, TG, BITS, 2>(ts, n, h, st, err);
+}
+
+template <class TP, class TG, int BITS>
+int rows_as(const smore_adamw_tensor& x, const Hyper& h, double* partial, hipStream_t st, const char** err)
 {
     RowsTensor r{};
     r.t = Tensor{x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, 0, 0, x.index, x.weight_decay};
@@ -498,7 +588,8 @@ int rows_as(const smore_adamw_tensor& x, const Hyper& h, float* partial, hipStre
     r.n_rows = x.n_rows;
     r.dim = x.dim;
     r.n_entries = x.n_entries;
-    r.per = x.per;
+    r.per = (uint32_t)(x.per < (1 << 30) ? x.per : 1 << 30);   // entries are fewer
+    r.per_inverse = 1.0 / r.per;
     const int64_t sums = x.n_entries / RUN;
     if (sums) k_run_sums<TG><<<(unsigned)((sums + WAVES - 1) / WAVES), WG, 0, st>>>(r, partial);
     if (x.n_entries) k_adamw_rows<TP, TG, BITS><<<(unsigned)((x.n_entries + WAVES - 1) / WAVES), WG, 0, st>>>(r, h);
@@ -526,7 +617,7 @@ size_t adamw_workspace(const smore_adamw_tensor* ts, int n)
 {
     size_t most = 0;   // tensors of a call are stepped one after the other
     for (int k = 0; k < n; ++k) {
-        const size_t need = ts[k].rows ? (size_t)(ts[k].n_entries / RUN) * ts[k].dim * sizeof(float) : 0;
+        const size_t need = ts[k].rows ? (size_t)(ts[k].n_entries / RUN) * ts[k].dim * sizeof(double) : 0;
         most = need > most ? need : most;
     }
     return most;
@@ -535,26 +626,30 @@ size_t adamw_workspace(const smore_adamw_tensor* ts, int n)
 int launch_adamw(const smore_adamw_tensor* ts, int n, const smore_adamw_args& a, void* ws, hipStream_t st, const char** err)
 {
     Hyper h{};
-    h.lr = (float)a.lr;
-    h.b1 = (float)a.beta1;
-    h.b2 = (float)a.beta2;
-    h.eps = (float)a.eps;
+    h.s.rate = (float)a.lr;
+    h.s.b1 = (float)a.beta1;
+    h.s.b2 = (float)a.beta2;
+    h.s.a1 = (float)(1.0 - a.beta1);
+    h.s.a2 = (float)(1.0 - a.beta2);
+    h.s.eps = (float)a.eps;
+    h.s.move = (float)((a.lr_device ? 1.0 : a.lr) / -expm1((double)a.step * log(a.beta1)));
+    h.s.root = (float)(1.0 / sqrt(-expm1((double)a.step * log(a.beta2))));
+    h.s.scale = 1.0f;
     h.log_b1 = (float)log(a.beta1);
     h.log_b2 = (float)log(a.beta2);
-    h.c1 = (float)-expm1((double)a.step * log(a.beta1));
-    h.c2 = (float)-expm1((double)a.step * log(a.beta2));
     h.step = a.step_device;
     h.lr_dev = a.lr_device;
     h.grad_scale = a.grad_scale;
-    h.step_host = a.step;
-    h.seed = a.seed;
+    h.on_device = a.step_device || a.lr_device || a.grad_scale;
+    h.seed_key = mix(mix((uint32_t)a.seed) ^ (uint32_t)(a.seed >> 32));
+    h.s.key = step_key(h.seed_key, a.step);
     h.stochastic = (a.flags & SMORE_ADAMW_STOCHASTIC) != 0;
     for (int k = 0; k < n;) {
         const smore_adamw_tensor& x = ts[k];
         int end = k + 1, rc;
         if (x.rows) {
             rc = by_type(x.param_type, x.grad_type, x.bits, [&](auto p, auto g, auto bits) {
-                return rows_as<decltype(p), decltype(g), decltype(bits)::value>(x, h, (float*)ws, st, err);
+                return rows_as<decltype(p), decltype(g), decltype(bits)::value>(x, h, (double*)ws, st, err);
             });
         } else {
             // dense tensors of the same types that follow each other go together
