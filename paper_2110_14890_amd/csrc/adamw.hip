@@ -146,31 +146,24 @@ __device__ __forceinline__ float second_moment(float v, float g, const Step& s)
     return kept + added;
 }
 
-// e4m3 (4 exponent bits of bias 7, 3 fraction bits, no infinity) is what is
-// left of fp32 times 2^-120 without its 20 lowest bits: the exponent's bias
-// moves from 127 to 7, and e4m3's subnormals below 2^-6 are fp32's below
-// 2^-126.  Rounding is an addition to those 20 bits, before they go; values
-// up to 448 (and a few half steps above) cannot be carried past 448.
-constexpr float TO_CODE = 0x1p-120f;
-constexpr float LEAST_CODE = 0x1p-129f;
-
-// Bits of a value (relative to its block's largest, times 448) whose bits 20
-// to 26, and 31, are its code.
-__device__ __forceinline__ uint32_t code_bits(float y, uint32_t draw, bool stochastic)
+// Codes of four values of [-448, 448].  The stochastic conversion adds its
+// word's high 20 bits to the 20 fraction bits that a code drops (below 2^-6:
+// to the fraction of 2^-9), of which a draw fills the upper 16.
+__device__ __forceinline__ uint32_t encode(const float* y, const uint32_t* draw, bool stochastic)
 {
-    const uint32_t bits = __float_as_uint(y);
-    return stochastic ? bits + (draw << 4) : bits + 0x7FFFFu + ((bits >> 20) & 1u);
+    int x = 0;
+    if (stochastic) {
+        x = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], (int)draw[0], x, 0);
+        x = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], (int)draw[1], x, 1);
+        x = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], (int)draw[2], x, 2);
+        x = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], (int)draw[3], x, 3);
+    } else {
+        x = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], x, false);
+        x = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], x, true);
+    }
+    return (uint32_t)x;
 }
-// Four codes of such bits: sign and magnitude moved to the top byte each,
-// then the top bytes gathered.
-__device__ __forceinline__ uint32_t gather_codes(const uint32_t* bits)
-{
-    uint32_t x[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = ((bits[j] << 4) & 0x7FFFFFFFu) | (bits[j] & 0x80000000u);
-    const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x0C0C0703u);   // bytes 3 of x[0] and x[1]
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(x[3], x[2], 0x07030C0Cu), lo, 0x07060100u);
-}
+constexpr float LEAST_CODE = 0x1p-9f;
 
 // Values of four codes.
 __device__ __forceinline__ void decode(uint32_t four, float* out)
@@ -196,11 +189,12 @@ __device__ __forceinline__ uint32_t block_max(uint32_t x)
     return x;
 }
 
-// Scale of a block and the factor that takes its values to [0, 448].
+// Scale of a block and the factor that takes its values to [0, 448].  Blocks
+// that have decayed below 2^-100 are 0, which keeps the factor finite.
 __device__ __forceinline__ void block_scale(uint32_t top_bits, float* scale, float* unit)
 {
     const float top = __uint_as_float(top_bits);
-    const bool some = top >= 1.17549435e-38f;
+    const bool some = top >= 0x1p-100f;
     *scale = top_bits >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : some ? top * (1.0f / 448.0f) : 0.0f;
     *unit = some ? (1.0f / top) * 448.0f : 0.0f;
 }
@@ -277,9 +271,13 @@ __device__ __forceinline__ void load_held(const Tensor& t, int64_t at, int64_t h
 // first element in its block.
 template <class TP, int BITS>
 __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool stochastic, int64_t at, int64_t have,
-                                          int64_t block, int j0, float* p, const float* g, Held<BITS>& h)
+                                          int64_t block, int j0, float* p, float* g, Held<BITS>& h)
 {
     float m[PER], v[PER], u[PER];
+    if (s.scale != 1.0f) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) g[j] *= s.scale;
+    }
     if constexpr (BITS == 32) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
@@ -301,9 +299,8 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        const float gj = g[j] * s.scale;
-        m[j] = first_moment(m[j], gj, s);
-        v[j] = second_moment(v[j], gj, s);
+        m[j] = first_moment(m[j], g[j], s);
+        v[j] = second_moment(v[j], g[j], s);
         u[j] = BITS == 8 ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
         p[j] = fmaf(-s.move * m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.root, s.eps)), p[j] * s.keep);
     }
@@ -347,21 +344,35 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
         float m_scale, m_unit, u_scale, u_unit;
         block_scale(block_max(m_top), &m_scale, &m_unit);
         block_scale(block_max(u_top), &u_scale, &u_unit);
-        uint32_t mc[PER], uc[PER];
+        float least = 448.0f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            mc[j] = code_bits((m[j] * m_unit) * TO_CODE, draw[j] & 0xFFFFu, stochastic);
-            // a root that is not 0 has a code that is not 0
-            const uint32_t low = u[j] != 0.0f && u_unit > 0.0f ? __float_as_uint(LEAST_CODE) : 0u;
-            uc[j] = max(code_bits((u[j] * u_unit) * TO_CODE, draw[j] >> 16, stochastic), low);
+            m[j] *= m_unit;
+            const float y = u[j] * u_unit;
+            least = fminf(least, y);
+            p[j] = u[j];      // the parameter is written: its place keeps the root
+            u[j] = y;
+        }
+        // a root that is not 0 has a code that is not 0 (rarely below it: a
+        // root under 2^-18 of its block's largest)
+        if (__any(least < LEAST_CODE)) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (p[j] != 0.0f && u_unit > 0.0f) u[j] = fmaxf(u[j], LEAST_CODE);
+        }
+        uint32_t low[PER], high[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            low[j] = draw[j] << 16;
+            high[j] = draw[j] & 0xFFFF0000u;
+        }
+        uint32_t m4[PER / 4], u4[PER / 4];
+#pragma unroll
+        for (int k = 0; k < PER / 4; ++k) {
+            m4[k] = encode(m + 4 * k, low + 4 * k, stochastic);
+            u4[k] = encode(u + 4 * k, high + 4 * k, stochastic);
         }
         if (have > 0) {
-            uint32_t m4[PER / 4], u4[PER / 4];
-#pragma unroll
-            for (int k = 0; k < PER / 4; ++k) {
-                m4[k] = gather_codes(mc + 4 * k);
-                u4[k] = gather_codes(uc + 4 * k);
-            }
             store_codes((uint8_t*)t.m + at, have, m4);
             store_codes((uint8_t*)t.v + at, have, u4);
             if (j0 == 0) {
