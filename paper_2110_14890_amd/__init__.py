@@ -505,88 +505,96 @@ def gather_probe(table, n_reads: int, stream=None):
 
 
 # ------------------------------------------------- training on sampled batches
-def _types() -> dict:
-    import torch
-    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+# Small calls take as long as this binding does, so the checks of a call are
+# plain comparisons; what is wrong is spelled out only where one fails.
+_torch = None
+_TYPES = {}          # element types of the C ABI
 
 
-class _Launch:
-    """The device of a call's tensors made current, and its stream: the given
-    one, or the device's current stream.  Tensors made inside belong to that
-    stream."""
-
-    def __init__(self, device, stream):
+def _lazy_torch():
+    global _torch
+    if _torch is None:
         import torch
-        if device.type != "cuda":
-            raise ValueError(f"tensors must be on a GPU, not on {device}")
-        if stream is not None and stream.device != device:
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _torch = torch
+    return _torch
+
+
+def _launch(device, stream, call):
+    """call(stream handle) with the device current and its stream: the given
+    one, or the device's current stream.  Tensors that call makes belong to
+    that stream."""
+    torch = _torch
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, not on {device}")
+    if stream is not None:
+        if stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-        self._guard = None
-        if stream is not None:
-            self._guard = torch.cuda.stream(stream)
-        elif torch.cuda.current_device() != device.index:
-            self._guard = torch.cuda.device(device)
-        self.handle = c_vp((stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream)
-
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-        return self.handle
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
+    if torch.cuda.current_device() == device.index:
+        return call(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return call(torch.cuda.current_stream(device).cuda_stream)
 
 
-def _operand(name: str, t, shape: tuple, dtypes, device) -> None:
-    """A device tensor of this shape and one of these types whose rows are
-    contiguous (the distance of two rows is free)."""
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+def _fits(t, shape, dtype, device) -> bool:
+    """A tensor of this shape, type and device whose rows are contiguous (the
+    distance of two rows is free)."""
+    return t.shape == shape and t.dtype == dtype and t.device == device and \
+        (len(shape) < 2 or shape[1] < 2 or t.stride(1) == 1)
+
+
+def _operand(name: str, t, shape, dtypes, device) -> None:
+    """Says what of _fits() does not hold."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
-    if t.device != device or t.device.type != "cuda":
-        raise ValueError(f"{name} must be on the GPU of the other tensors ({device}), it is on {t.device}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on the device of the other tensors ({device}), it is on {t.device}")
     if len(shape) == 2 and shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"rows of {name} must be contiguous")
 
 
-def _pitch(t) -> int:
-    """Distance of two rows of a matrix (a length for a single row)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _pitch(t, length: int) -> int:
+    """Distance of two rows of a matrix (its length for a single row)."""
+    return t.stride(0) if t.shape[0] > 1 else length
 
 
 def _ptr(t):
     return t.data_ptr() if t is not None and t.numel() else None
 
 
-def _score_args(table, candidates, query_type, query_pitch: int, score_pitch: int) -> ScoreArgs:
-    v, dim = table.shape
-    batch, n = candidates.shape
-    # one set for all queries: rows that coincide
-    pitch = candidates.stride(0) if batch > 1 else 0
-    return ScoreArgs(batch, n, dim, v, _pitch(table), query_pitch, pitch, score_pitch,
-                     _types()[table.dtype], _types()[query_type])
-
-
-def _check_table(table, candidates) -> None:
-    import torch
+def _score_args(table, candidates, other, other_name: str, grad_scores, grad_name: str) -> ScoreArgs:
+    """Checks and sizes of a score call: other [batch, dim], grad_scores [batch, n]."""
+    torch = _torch
     if table.dim() != 2 or candidates.dim() != 2:
         raise ValueError("table and candidates must be matrices")
+    v, dim = table.shape
+    shape = candidates.shape
+    batch, n = shape
+    device, te, tq = table.device, table.dtype, other.dtype
     wide = (torch.float32, torch.bfloat16)
-    _operand("table", table, tuple(table.shape), wide, table.device)
-    _operand("candidates", candidates, tuple(candidates.shape), (torch.int32,), table.device)
+    if not (te in wide and tq in wide and _fits(table, table.shape, te, device)
+            and _fits(candidates, shape, torch.int32, device) and _fits(other, (batch, dim), tq, device)
+            and _fits(grad_scores, shape, torch.float32, device)):
+        _operand("table", table, table.shape, wide, device)
+        _operand("candidates", candidates, shape, (torch.int32,), device)
+        _operand(other_name, other, (batch, dim), wide, device)
+        _operand(grad_name, grad_scores, shape, (torch.float32,), device)
+    if batch > 1:     # rows of the candidates may coincide: one set for all queries
+        return ScoreArgs(batch, n, dim, v, _pitch(table, dim), other.stride(0), candidates.stride(0),
+                         grad_scores.stride(0), _TYPES[te], _TYPES[tq])
+    return ScoreArgs(batch, n, dim, v, _pitch(table, dim), dim, n, n, _TYPES[te], _TYPES[tq])
 
 
 def score_into(table, queries, candidates, scores, stream=None):
     """smore_score into the caller's fp32 tensor [batch, n]."""
-    import torch
-    _check_table(table, candidates)
-    _operand("queries", queries, (candidates.shape[0], table.shape[1]), (torch.float32, torch.bfloat16), table.device)
-    _operand("scores", scores, tuple(candidates.shape), (torch.float32,), table.device)
-    args = _score_args(table, candidates, queries.dtype, _pitch(queries), _pitch(scores))
-    with _Launch(table.device, stream) as st:
-        _check(lib().smore_score(ctypes.byref(args), _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st))
+    _lazy_torch()
+    args = _score_args(table, candidates, queries, "queries", scores, "scores")
+    _check(_launch(table.device, stream, lambda st: lib().smore_score(
+        ctypes.byref(args), _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st)))
     return scores
 
 
@@ -596,27 +604,27 @@ def score(table, queries, candidates, stream=None):
     table [V, dim], 0 for candidates outside [0, V) (smore_score).  For one
     candidate set shared by all queries, candidates.expand(batch, n) works,
     but a matrix product with the set's rows is the faster way."""
-    import torch
-    with _Launch(table.device, stream):
-        scores = torch.empty(tuple(candidates.shape), dtype=torch.float32, device=table.device)
+    torch = _lazy_torch()
+    new = lambda _: torch.empty(candidates.shape, dtype=torch.float32, device=table.device)
+    scores = new(None) if stream is None else _launch(table.device, stream, new)
     return score_into(table, queries, candidates, scores, stream)
 
 
 def score_grad_into(table, candidates, grad_scores, grad_queries, stream=None):
     """smore_score_grad into the caller's tensor [batch, dim]."""
-    import torch
-    _check_table(table, candidates)
-    batch = candidates.shape[0]
-    _operand("grad_scores", grad_scores, tuple(candidates.shape), (torch.float32,), table.device)
-    _operand("grad_queries", grad_queries, (batch, table.shape[1]), (torch.float32, torch.bfloat16), table.device)
-    args = _score_args(table, candidates, grad_queries.dtype, _pitch(grad_queries), _pitch(grad_scores))
-    need = ctypes.c_size_t()
-    _check(lib().smore_score_grad_workspace_bytes(ctypes.byref(args), ctypes.byref(need)))
-    with _Launch(table.device, stream) as st:
-        # of this call alone, from the stream's (or the capturing graph's) memory
-        ws = torch.empty(need.value, dtype=torch.uint8, device=table.device) if need.value else None
-        _check(lib().smore_score_grad(ctypes.byref(args), _ptr(table), _ptr(candidates), _ptr(grad_scores),
-                                      _ptr(grad_queries), _ptr(ws), need.value, st))
+    torch = _lazy_torch()
+    args = _score_args(table, candidates, grad_queries, "grad_queries", grad_scores, "grad_scores")
+    L, need = lib(), ctypes.c_size_t()
+    _check(L.smore_score_grad_workspace_bytes(ctypes.byref(args), ctypes.byref(need)))
+    need = need.value
+
+    def call(st):
+        # a workspace of this call alone, from the stream's (or the capturing graph's) memory
+        ws = torch.empty(need, dtype=torch.uint8, device=table.device) if need else None
+        return L.smore_score_grad(ctypes.byref(args), _ptr(table), _ptr(candidates), _ptr(grad_scores),
+                                  _ptr(grad_queries), _ptr(ws), need, st)
+
+    _check(_launch(table.device, stream, call))
     return grad_queries
 
 
@@ -624,10 +632,26 @@ def score_grad(table, candidates, grad_scores, dtype=None, stream=None):
     """Gradient of score() for the queries, [batch, dim] in dtype (fp32): the
     sum of the candidates' rows, each times its entry of grad_scores (fp32
     [batch, n]).  The gradient for the table is AdamW's: row_grad()."""
-    import torch
-    with _Launch(table.device, stream):
-        out = torch.empty((candidates.shape[0], table.shape[1]), dtype=dtype or torch.float32, device=table.device)
+    torch = _lazy_torch()
+    new = lambda _: torch.empty((candidates.shape[0], table.shape[1]), dtype=dtype or torch.float32, device=table.device)
+    out = new(None) if stream is None else _launch(table.device, stream, new)
     return score_grad_into(table, candidates, grad_scores, out, stream)
+
+
+def _check_preference(batch, n, dtype, device, tensors: dict, vectors: dict) -> None:
+    """Says what is wrong with the tensors of a preference_loss call."""
+    torch = _torch
+    if dtype not in _TYPES:
+        raise ValueError(f"scores must be fp32, bf16 or fp16, got {dtype}")
+    for name, t in tensors.items():
+        if t is not None:
+            _operand(name, t, (batch, n) if "negatives" in name else (batch,), (dtype,), device)
+    for name, t in vectors.items():
+        if t is not None:
+            _operand(name, t, (batch, (n + 31) // 32) if name == "mask" else (batch,),
+                     (torch.int32,) if name in ("n_valid", "mask") else (torch.float32,), device)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
 
 
 def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_negatives=None, n_valid=None,
@@ -636,45 +660,53 @@ def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_
     """smore_preference_loss into the caller's tensors: out has "loss" (fp32
     [batch]), or "grad_positive" [batch] and "grad_negatives" [batch, n] of
     the scores' type, or all three."""
-    import torch
-    if kind not in PREFERENCE_KINDS:
+    torch = _lazy_torch()
+    number = PREFERENCE_KINDS.get(kind)
+    if number is None:
         raise ValueError(f"kind must be one of {sorted(PREFERENCE_KINDS)}, got {kind!r}")
     if negatives.dim() != 2:
         raise ValueError("negatives must be a matrix")
-    batch, n = negatives.shape
+    shape = negatives.shape
+    batch, n = shape
     device, dtype = negatives.device, negatives.dtype
-    if dtype not in _types():
-        raise ValueError(f"scores must be fp32, bf16 or fp16, got {dtype}")
+    loss, grad_p, grad_n = out.get("loss"), out.get("grad_positive"), out.get("grad_negatives")
     if (ref_positive is None) != (ref_negatives is None):
         raise ValueError("reference scores are given for both, or for neither")
-    grads = [out.get("grad_positive"), out.get("grad_negatives")]
-    if (grads[0] is None) != (grads[1] is None):
+    if (grad_p is None) != (grad_n is None):
         raise ValueError("gradients are wanted for both, or for neither")
-    for name, t, shape, types in (("positive", positive, (batch,), (dtype,)), ("negatives", negatives, (batch, n), (dtype,)),
-                                  ("ref_positive", ref_positive, (batch,), (dtype,)),
-                                  ("ref_negatives", ref_negatives, (batch, n), (dtype,)),
-                                  ("n_valid", n_valid, (batch,), (torch.int32,)),
-                                  ("mask", mask, (batch, (n + 31) // 32), (torch.int32,)),
-                                  ("loss", out.get("loss"), (batch,), (torch.float32,)),
-                                  ("grad_positive", grads[0], (batch,), (dtype,)),
-                                  ("grad_negatives", grads[1], (batch, n), (dtype,))):
-        if t is not None:
-            _operand(name, t, shape, types, device)
     scale = 1.0
     if weight is not None and not isinstance(weight, torch.Tensor):
         scale, weight = float(weight), None
+    row, i32, f32 = (batch,), torch.int32, torch.float32
+    good = dtype in _TYPES and _fits(positive, row, dtype, device) and (n < 2 or negatives.stride(1) == 1) \
+        and (ref_positive is None or (_fits(ref_positive, row, dtype, device) and _fits(ref_negatives, shape, dtype, device))) \
+        and (n_valid is None or (_fits(n_valid, row, i32, device) and n_valid.is_contiguous())) \
+        and (mask is None or (_fits(mask, (batch, (n + 31) // 32), i32, device) and mask.is_contiguous())) \
+        and (weight is None or (_fits(weight, row, f32, device) and weight.is_contiguous())) \
+        and (loss is None or (_fits(loss, row, f32, device) and loss.is_contiguous())) \
+        and (grad_p is None or (_fits(grad_p, row, dtype, device) and _fits(grad_n, shape, dtype, device)))
+    if not good:
+        _check_preference(batch, n, dtype, device,
+                          {"positive": positive, "negatives": negatives, "ref_positive": ref_positive,
+                           "ref_negatives": ref_negatives, "grad_positive": grad_p, "grad_negatives": grad_n},
+                          {"n_valid": n_valid, "mask": mask, "weight": weight, "loss": loss})
+    args = PreferenceArgs(batch, n, number, _TYPES[dtype], beta, smoothing, scale, positive.stride(0), negatives.stride(0))
+    ins = PreferenceIn(positive.data_ptr(), _ptr(negatives))
+    if ref_positive is not None:
+        args.ref_positive_stride, args.ref_negatives_stride = ref_positive.stride(0), ref_negatives.stride(0)
+        ins.ref_positive, ins.ref_negatives = ref_positive.data_ptr(), _ptr(ref_negatives)
+    if n_valid is not None:
+        ins.n_valid = n_valid.data_ptr()
+    if mask is not None:
+        ins.mask = _ptr(mask)
     if weight is not None:
-        _operand("weight", weight, (batch,), (torch.float32,), device)
-    for name, t in (("n_valid", n_valid), ("mask", mask), ("weight", weight), ("loss", out.get("loss"))):
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    row = lambda t: 0 if t is None else t.stride(0) if batch > 1 else n
-    args = PreferenceArgs(batch, n, PREFERENCE_KINDS[kind], _types()[dtype], beta, smoothing, scale, row(positive),
-                          row(negatives), row(ref_positive), row(ref_negatives), row(grads[0]), row(grads[1]))
-    ins = PreferenceIn(*[_ptr(t) for t in (positive, negatives, ref_positive, ref_negatives, n_valid, mask, weight)])
-    outs = PreferenceOut(*[_ptr(t) for t in (out.get("loss"), *grads)])
-    with _Launch(device, stream) as st:
-        _check(lib().smore_preference_loss(ctypes.byref(args), ctypes.byref(ins), ctypes.byref(outs), st))
+        ins.weight = weight.data_ptr()
+    outs = PreferenceOut(loss.data_ptr() if loss is not None else None)
+    if grad_p is not None:
+        args.grad_positive_stride, args.grad_negatives_stride = grad_p.stride(0), grad_n.stride(0)
+        outs.grad_positive, outs.grad_negatives = grad_p.data_ptr(), _ptr(grad_n)
+    _check(_launch(device, stream, lambda st: lib().smore_preference_loss(
+        ctypes.byref(args), ctypes.byref(ins), ctypes.byref(outs), st)))
     return out
 
 
@@ -691,13 +723,17 @@ def preference_loss(positive, negatives, ref_positive=None, ref_negatives=None, 
     takes the positive against all negatives at once.  The formulas stand at
     smore_preference_loss.  Scores may be views of one matrix (a column, the
     columns behind it)."""
-    import torch
-    with _Launch(negatives.device, stream):
-        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=negatives.device)
-        out = {"loss": new(negatives.shape[:1], torch.float32)}
+    torch = _lazy_torch()
+
+    def new(_):
+        rows, device = negatives.shape[:1], negatives.device
+        out = {"loss": torch.empty(rows, dtype=torch.float32, device=device)}
         if grad:
-            out["grad_positive"] = new(negatives.shape[:1], negatives.dtype)
-            out["grad_negatives"] = new(tuple(negatives.shape), negatives.dtype)
+            out["grad_positive"] = torch.empty(rows, dtype=negatives.dtype, device=device)
+            out["grad_negatives"] = torch.empty(negatives.shape, dtype=negatives.dtype, device=device)
+        return out
+
+    out = new(None) if stream is None else _launch(negatives.device, stream, new)
     return preference_loss_into(positive, negatives, out, ref_positive, ref_negatives, n_valid, mask, kind, beta,
                                 smoothing, weight, stream)
 
@@ -717,8 +753,7 @@ def row_grad(ids, grad, coef=None, per: int = 1) -> RowGrad:
     the flattened ids, adds coef[i] times grad[i // per].  With score()'s
     candidates [batch, n] as ids, its queries as grad, the gradient of its
     scores as coef and per = n this is score()'s gradient for the table."""
-    import torch
-    rows, order = torch.sort(ids.reshape(-1), stable=True)
+    rows, order = _lazy_torch().sort(ids.reshape(-1), stable=True)
     return RowGrad(rows, grad, order, None if coef is None else coef.reshape(-1), per)
 
 
@@ -727,7 +762,7 @@ def alloc_adamw_state(param, bits: int = 32, table: bool = False) -> dict:
     bits float8_e4m3fn codes of m and sqrt(v) with fp32 scales "m_scale",
     "v_scale" per block of ADAMW_BLOCK elements: of each row for a table
     [V, dim] whose rows are stepped, else of the parameter as one row."""
-    import torch
+    torch = _lazy_torch()
     new = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=param.device)
     if bits == 32:
         return {k: new(tuple(param.shape), torch.float32) for k in ("m", "v")}
@@ -757,7 +792,7 @@ class AdamW:
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  bits: int = 32, seed: "int | None" = None, tables=(), states=None, steps: int = 0,
                  device_step: bool = False):
-        import torch
+        torch = _lazy_torch()
         self.params = list(params)
         self.lr, self.betas, self.eps, self.seed, self.steps = lr, betas, eps, seed, steps
         self.weight_decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else \
@@ -771,17 +806,20 @@ class AdamW:
         if states is None:
             states = [alloc_adamw_state(p, bits, k in tables) for k, p in enumerate(self.params)]
         self.states, self.bits = list(states), bits
-        self.device_steps = torch.full((1,), steps, dtype=torch.int64, device=self.device) if device_step else None
         if len(self.states) != len(self.params):
             raise ValueError("one state per parameter is needed")
-        self._list = (AdamWTensor * len(self.params))()
-        self._seen = [None] * len(self.params)
-        for k in range(len(self.params)):
+        self.device_steps = torch.full((1,), steps, dtype=torch.int64, device=self.device) if device_step else None
+        # what the library gets for each parameter, the addresses it was made for,
+        # whether scales allow steps by rows and of the whole, and its last gradient's type
+        n = len(self.params)
+        self._list = (AdamWTensor * n)()
+        self._seen, self._by_rows, self._whole, self._last = [None] * n, [True] * n, [True] * n, [None] * n
+        for k in range(n):
             self._describe(k)
 
     def _describe(self, k: int) -> None:
         """Checks parameter k and its moments and puts them into the list."""
-        import torch
+        torch = _torch
         p, state = self.params[k], self.states[k]
         if p.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"parameter {k} must be fp32 or bf16, got {p.dtype}")
@@ -811,8 +849,9 @@ class AdamW:
         x.param, x.m, x.v = p.data_ptr(), state["m"].data_ptr(), state["v"].data_ptr()
         x.m_scale, x.v_scale = (state["m_scale"].data_ptr(), state["v_scale"].data_ptr()) if self.bits == 8 else (None, None)
         x.n_rows, x.dim = (p.shape[0], p.shape[1]) if p.dim() == 2 else (1, p.numel())
-        x.param_type, x.bits, x.index, x.weight_decay = _types()[p.dtype], self.bits, k, self.weight_decay[k]
-        self._seen[k] = (tuple(t.data_ptr() for t in (p, *(state[n] for n in shapes))), p.shape, by_rows, whole)
+        x.param_type, x.bits, x.index, x.weight_decay = _TYPES[p.dtype], self.bits, k, self.weight_decay[k]
+        self._seen[k] = [p.shape, p] + [t.data_ptr() for t in (p, *(state[n] for n in shapes))]
+        self._by_rows[k], self._whole[k], self._last[k] = by_rows, whole, None
 
     def step(self, grads, grad_scale=None, stream=None) -> None:
         """One step.  grads: for each parameter a contiguous tensor of its
@@ -820,31 +859,36 @@ class AdamW:
         it.  grad_scale: an fp32 device tensor [1] that multiplies every
         gradient (of a norm's clipping, of a scaled loss); nothing is written
         where it is not finite, though the step counts."""
-        import torch
+        torch = _torch
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        types, used = _types(), []
-        for k, (p, g) in enumerate(zip(self.params, grads)):
+        used, device, scaled = [], self.device, self.bits == 8
+        for k, g in enumerate(grads):
             if g is None:
                 continue
-            if p.numel() == 0:
-                continue
-            state = self.states[k]
-            seen = self._seen[k]
-            if seen[0][:3] != (p.data_ptr(), state["m"].data_ptr(), state["v"].data_ptr()) or seen[1] != p.shape:
+            p, state, seen = self.params[k], self.states[k], self._seen[k]
+            shape = p.shape
+            # a parameter or moments that were replaced are looked at again
+            if p is not seen[1] or shape != seen[0] or p.data_ptr() != seen[2] or state["m"].data_ptr() != seen[3] \
+                    or state["v"].data_ptr() != seen[4] or (scaled and (state["m_scale"].data_ptr() != seen[5]
+                                                                        or state["v_scale"].data_ptr() != seen[6])):
                 self._describe(k)
-                seen = self._seen[k]
-            x = self._list[k]
-            if isinstance(g, RowGrad):
-                self._rows(k, x, p, g, seen[2], types)
+            if type(g) is RowGrad:
+                self._rows(k, self._list[k], p, g)
             else:
-                if g.dtype not in types or g.shape != p.shape or g.device != self.device or not g.is_contiguous():
-                    raise ValueError(f"gradient {k} must be a contiguous tensor of shape {tuple(p.shape)} on {self.device}, "
+                if g.shape != shape or g.dtype not in _TYPES or g.device != device or not g.is_contiguous():
+                    raise ValueError(f"gradient {k} must be a contiguous tensor of shape {tuple(shape)} on {device}, "
                                      f"got {g.dtype} {tuple(g.shape)} on {g.device}")
-                if not seen[3]:
-                    raise ValueError(f"the moments of parameter {k} have scales per row: its gradient must be a RowGrad")
-                x.grad, x.grad_type, x.rows, x.order, x.coef = g.data_ptr(), types[g.dtype], None, None, None
+                x = self._list[k]
+                x.grad = g.data_ptr()
+                if self._last[k] is not g.dtype:
+                    if not self._whole[k]:
+                        raise ValueError(f"the moments of parameter {k} have scales per row: its gradient must be a RowGrad")
+                    x.grad_type, x.rows, x.order, x.coef = _TYPES[g.dtype], None, None, None
+                    self._last[k] = g.dtype
+                if not shape.numel():
+                    continue
             used.append(k)
         for name, t, dtype in (("lr", self.lr if isinstance(self.lr, torch.Tensor) else None, torch.float32),
                                ("grad_scale", grad_scale, torch.float32)):
@@ -858,23 +902,30 @@ class AdamW:
         args = AdamWArgs(0.0 if device_lr else self.lr, self.betas[0], self.betas[1], self.eps, self.steps + 1,
                          _ptr(self.device_steps), self.lr.data_ptr() if device_lr else None, _ptr(grad_scale),
                          0 if self.seed is None else self.seed, 0 if self.seed is None else ADAMW_STOCHASTIC)
-        need = ctypes.c_size_t()
-        _check(lib().smore_adamw_workspace_bytes(ts, len(used), ctypes.byref(need)))
-        with _Launch(self.device, stream) as st:
-            ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+        L, n, need = lib(), len(used), 0
+        if any(type(grads[k]) is RowGrad for k in used):
+            size = ctypes.c_size_t()
+            _check(L.smore_adamw_workspace_bytes(ts, n, ctypes.byref(size)))
+            need = size.value
+
+        def call(st):
+            # a workspace of this call alone, from the stream's (or the capturing graph's) memory
+            ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
             if self.device_steps is not None:
                 self.device_steps.add_(1)
-            rc = lib().smore_adamw(ts, len(used), ctypes.byref(args), _ptr(ws), need.value, st)
+            rc = L.smore_adamw(ts, n, ctypes.byref(args), _ptr(ws), need, st)
             if rc and self.device_steps is not None:
                 self.device_steps.sub_(1)
-            _check(rc)
+            return rc
+
+        _check(_launch(device, stream, call))
         self.steps += 1
         # autograd sees that they changed
         torch.autograd.graph.increment_version([self.params[k] for k in used if not self.params[k].is_inference()])
 
-    def _rows(self, k: int, x, p, g: RowGrad, by_rows: bool, types: dict) -> None:
-        import torch
-        if p.dim() != 2 or not by_rows:
+    def _rows(self, k: int, x, p, g: RowGrad) -> None:
+        torch = _torch
+        if p.dim() != 2 or not self._by_rows[k]:
             raise ValueError(f"parameter {k} is no table with moments per row: its gradient cannot be a RowGrad")
         n = g.rows.numel()
         ok = lambda t, dtype, numel: t.dtype == dtype and t.device == self.device and t.is_contiguous() and t.numel() == numel
@@ -885,9 +936,9 @@ class AdamW:
         if g.coef is not None and not ok(g.coef, torch.float32, n):
             raise ValueError(f"coef of gradient {k} must be a contiguous fp32 tensor of {n} entries on {self.device}")
         if g.per < 1 or g.grad.dim() != 2 or g.grad.shape[1] != p.shape[1] or g.grad.shape[0] * g.per < n or \
-                g.grad.dtype not in types or g.grad.device != self.device or not g.grad.is_contiguous():
+                g.grad.dtype not in _TYPES or g.grad.device != self.device or not g.grad.is_contiguous():
             raise ValueError(f"gradient {k} must hold contiguous rows of {p.shape[1]} on {self.device}, one for each "
                              f"{g.per} of {n} entries, got {g.grad.dtype} {tuple(g.grad.shape)} on {g.grad.device}")
-        x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), types[g.grad.dtype], g.rows.data_ptr(), \
+        x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), _TYPES[g.grad.dtype], g.rows.data_ptr(), \
             None if g.order is None else g.order.data_ptr(), None if g.coef is None else g.coef.data_ptr()
-        x.n_entries, x.per = n, g.per
+        x.n_entries, x.per, self._last[k] = n, g.per, RowGrad

@@ -195,23 +195,37 @@ __device__ __forceinline__ void block_scale(uint32_t top_bits, float* scale, flo
 {
     const float top = __uint_as_float(top_bits);
     const bool some = top >= 0x1p-100f;
+    const float r = __builtin_amdgcn_rcpf(top);
     *scale = top_bits >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : some ? top * (1.0f / 448.0f) : 0.0f;
-    *unit = some ? (1.0f / top) * 448.0f : 0.0f;
+    // 1 / top to the nearest, as root_of()
+    *unit = some ? fmaf(fmaf(-top, r, 1.0f), r, r) * 448.0f : 0.0f;
 }
 
-// Parameters of a lane, rounded; bf16 stochastically by bits that are a
-// product's of the element's draw.
-__device__ __forceinline__ float to_param(float p, uint32_t, bool, float) { return p; }
-__device__ __forceinline__ bf16 to_param(float p, uint32_t draw, bool stochastic, bf16)
+// A lane's parameters to memory; bf16 rounded stochastically by bits that are
+// a product's of the element's draw.
+__device__ __forceinline__ void store_params(float* dst, int have, const float* p, const uint32_t*, bool)
 {
-    if (!stochastic) return (bf16)p;
-    const uint32_t up = ((draw ^ 0x85EBCA6Bu) * 0x9E3779B1u) >> 16;
-    const uint32_t bits = __float_as_uint(p);
-    // a NaN's lower bits could be carried into its sign
-    const uint16_t top = (uint16_t)((p == p ? bits + up : 0x7FC00000u) >> 16);
-    bf16 out;
-    __builtin_memcpy(&out, &top, sizeof(out));
-    return out;
+    store_floats<float, PER>(dst, have, p);
+}
+__device__ __forceinline__ void store_params(bf16* dst, int have, const float* p, const uint32_t* draw, bool stochastic)
+{
+    if (!stochastic) return store_floats<bf16, PER>(dst, have, p);
+    uint32_t x[PER / 2];
+#pragma unroll
+    for (int k = 0; k < PER / 2; ++k) {
+        const uint32_t lo = __float_as_uint(p[2 * k]) + (((draw[2 * k] ^ 0x85EBCA6Bu) * 0x9E3779B1u) >> 16);
+        const uint32_t hi = __float_as_uint(p[2 * k + 1]) + (((draw[2 * k + 1] ^ 0x85EBCA6Bu) * 0x9E3779B1u) >> 16);
+        x[k] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);   // their upper halves
+    }
+    if (have >= PER) {
+        __builtin_memcpy(dst, x, sizeof(x));
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER - 1; ++j) {
+            const uint16_t one = (uint16_t)(x[j / 2] >> (16 * (j % 2)));
+            if (j < have) __builtin_memcpy(dst + j, &one, 2);
+        }
+    }
 }
 
 // Elements and moments that a lane holds.
@@ -227,7 +241,7 @@ struct Held<8> {
     float m_scale, v_scale;
 };
 
-__device__ __forceinline__ void load_codes(const uint8_t* p, int64_t have, uint32_t* x)
+__device__ __forceinline__ void load_codes(const uint8_t* p, int have, uint32_t* x)
 {
     if (have >= PER) {
         __builtin_memcpy(x, p, PER);
@@ -239,7 +253,7 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, int64_t have, uint3
             if (j < have) x[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
     }
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t have, const uint32_t* x)
+__device__ __forceinline__ void store_codes(uint8_t* p, int have, const uint32_t* x)
 {
     if (have >= PER) {
         __builtin_memcpy(p, x, PER);
@@ -253,7 +267,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t have, const uint
 // at: the lane's first element in the tensor; have: how many of its PER
 // elements the row has (none: <= 0); block: number of its 128-element block.
 template <int BITS>
-__device__ __forceinline__ void load_held(const Tensor& t, int64_t at, int64_t have, int64_t block, Held<BITS>& h)
+__device__ __forceinline__ void load_held(const Tensor& t, int64_t at, int have, int64_t block, Held<BITS>& h)
 {
     if constexpr (BITS == 32) {
         load_floats<float, PER>((const float*)t.m + at, have, h.m);
@@ -270,7 +284,7 @@ __device__ __forceinline__ void load_held(const Tensor& t, int64_t at, int64_t h
 // wavefront takes part (the maxima of the 8-bit blocks).  j0: the lane's
 // first element in its block.
 template <class TP, int BITS>
-__device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool stochastic, int64_t at, int64_t have,
+__device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool stochastic, int64_t at, int have,
                                           int64_t block, int j0, float* p, float* g, Held<BITS>& h)
 {
     float m[PER], v[PER], u[PER];
@@ -311,36 +325,27 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
 #pragma unroll
         for (int j = 0; j < PER; ++j) draw[j] = mix(base + (uint32_t)j);
     }
-    if (have > 0) {
-        Vec<TP, PER> out;
+    // Adding to a NaN's lower bits could carry into its sign, and make it 0.
+    // A NaN of that kind comes with the gradient or the moments.
+    uint32_t m_top = 0;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) out.x[j] = to_param(p[j], draw[j], stochastic, TP{});
-        TP* dst = (TP*)t.p + at;
-        if (have >= PER) {
-            store_vec<TP, PER>(dst, out);
-        } else {
+    for (int j = 0; j < PER; ++j) m_top = max(m_top, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+    if (sizeof(TP) == 2 && stochastic && __any(m_top > 0x7F800000u)) {
 #pragma unroll
-            for (int j = 0; j < PER - 1; ++j)
-                if (j < have) dst[j] = out.x[j];
-        }
+        for (int j = 0; j < PER; ++j)
+            if (p[j] != p[j]) p[j] = __uint_as_float(0x7FC00000u);
     }
+    if (have > 0) store_params((TP*)t.p + at, have, p, draw, stochastic);
     if constexpr (BITS == 32) {
         if (have > 0) {
             store_floats<float, PER>((float*)t.m + at, have, m);
             store_floats<float, PER>((float*)t.v + at, have, v);
         }
     } else {
-        uint32_t m_top = 0, u_top = 0;
-        if (have < PER) {
+        // places behind the row's end were loaded as zeros and are 0 still
+        uint32_t u_top = 0;
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (j >= have) m[j] = u[j] = 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            m_top = max(m_top, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-            u_top = max(u_top, __float_as_uint(u[j]) & 0x7FFFFFFFu);
-        }
+        for (int j = 0; j < PER; ++j) u_top = max(u_top, __float_as_uint(u[j]) & 0x7FFFFFFFu);
         float m_scale, m_unit, u_scale, u_unit;
         block_scale(block_max(m_top), &m_scale, &m_unit);
         block_scale(block_max(u_top), &u_scale, &u_unit);
@@ -383,6 +388,9 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
     }
 }
 
+// How many of a lane's PER elements, from `at` on, lie before `end`.
+__device__ __forceinline__ int left(int64_t end, int64_t at) { return (int)max((int64_t)0, min((int64_t)PER, end - at)); }
+
 // A workgroup takes WAVES x CHUNKS chunks of one tensor; which one it finds
 // among the launch's tensors by their first workgroups.
 template <class TP, class TG, int BITS, int CHUNKS>
@@ -404,7 +412,8 @@ __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper
     Held<BITS> h[CHUNKS];
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const int64_t at = base + c * CHUNK, have = t.count - at;
+        const int64_t at = base + c * CHUNK;
+        const int have = left(t.count, at);
         load_floats<TP, PER>((const TP*)t.p + at, have, p[c]);
         load_floats<TG, PER>((const TG*)t.g + at, have, g[c]);
         load_held<BITS>(t, at, have, at / BLOCK, h[c]);
@@ -412,7 +421,7 @@ __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int64_t at = base + c * CHUNK;
-        step_held<TP, BITS>(t, s, stochastic, at, t.count - at, at / BLOCK, (int)(at % BLOCK), p[c], g[c], h[c]);
+        step_held<TP, BITS>(t, s, stochastic, at, left(t.count, at), at / BLOCK, (int)(at % BLOCK), p[c], g[c], h[c]);
     }
 }
 
@@ -441,7 +450,7 @@ __device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64
 // Adds the entries [first, end): products in fp32, their sum in 64 bits, so
 // that long runs lose nothing and the order does not show.
 template <class TG>
-__device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, int64_t end, int64_t col, int64_t have,
+__device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, int64_t end, int64_t col, int have,
                                             double* g)
 {
     const int lane = threadIdx.x & 63;
@@ -470,7 +479,7 @@ __global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, double* __r
     const int32_t row = r.rows[c * RUN];
     if (row < 0 || row >= r.n_rows || r.rows[c * RUN + RUN - 1] != row) return;
     for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
-        const int64_t have = r.dim - col;
+        const int have = left(r.dim, col);
         double g[PER] = {};
         add_entries<TG>(r, c * RUN, (c + 1) * RUN, col, have, g);
 #pragma unroll
@@ -527,7 +536,8 @@ __global__ __launch_bounds__(WG) void k_adamw_rows(const RowsTensor r, const Hyp
     }
     const int64_t blocks = (r.dim + BLOCK - 1) / BLOCK;
     for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
-        const int64_t have = r.dim - col, at = (int64_t)row * r.dim + col, block = row * blocks + col / BLOCK;
+        const int have = left(r.dim, col);
+        const int64_t at = (int64_t)row * r.dim + col, block = row * blocks + col / BLOCK;
         float p[PER], g[PER];
         Held<BITS> h;
         load_floats<TP, PER>((const TP*)r.t.p + at, have, p);

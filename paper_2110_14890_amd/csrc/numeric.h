@@ -34,7 +34,7 @@ __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v)
 // The first `count` of V elements at p as floats, 0 for the others; none of
 // them is read.
 template <class T, int V>
-__device__ __forceinline__ void load_floats(const T* p, int64_t count, float* out)
+__device__ __forceinline__ void load_floats(const T* p, int count, float* out)
 {
     if (count >= V) {
         const Vec<T, V> v = load_vec<T, V>(p);
@@ -46,7 +46,7 @@ __device__ __forceinline__ void load_floats(const T* p, int64_t count, float* ou
     }
 }
 template <class T, int V>
-__device__ __forceinline__ void store_floats(T* p, int64_t count, const float* in)
+__device__ __forceinline__ void store_floats(T* p, int count, const float* in)
 {
     if (count >= V) {
         Vec<T, V> v;

@@ -20,9 +20,9 @@ namespace {
 constexpr int WG = 256;
 constexpr int WAVES = WG / 64;
 
-// Columns [first, first + V) of a row that a lane holds in register block i,
-// LANES lanes per row.  The last block of a row that is no multiple of V is
-// moved back to end with the row: `skip` of its columns belong to the lane
+// Columns that a lane holds in register block i of a row, LANES lanes per
+// row: V from `first` on.  The last block of a row that is no multiple of V
+// is moved back to end with the row; `skip` of its columns belong to the lane
 // before.  Rows shorter than V take V = 1.
 template <int LANES, int V>
 struct Columns {
@@ -37,7 +37,24 @@ struct Columns {
     }
 };
 
-// Elements of a row that a lane holds, as floats; columns of another lane 0.
+// The register blocks of U rows.  All loads of a block stand in one branch,
+// so that they are in flight together.
+template <class T, int LANES, int V, int NI, int U>
+__device__ __forceinline__ void fetch(const T* const* rows, int lane, int tile0, int dim, Vec<T, V> (*raw)[NI])
+{
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const Columns<LANES, V> at(lane, i, tile0, dim);
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u][i] = Vec<T, V>{};
+        if (at.any) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u][i] = load_vec<T, V>(rows[u] + at.first);
+        }
+    }
+}
+
+// A row's register blocks as floats; columns of another lane 0.
 template <class T, int LANES, int V, int NI>
 __device__ __forceinline__ void take(const Vec<T, V>* raw, int lane, int tile0, int dim, bool ragged, float (*out)[V])
 {
@@ -53,83 +70,138 @@ __device__ __forceinline__ void take(const Vec<T, V>* raw, int lane, int tile0, 
     }
 }
 
-template <class T, int LANES, int V, int NI>
-__device__ __forceinline__ void fetch(const T* row, int lane, int tile0, int dim, bool real, Vec<T, V>* raw)
-{
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const Columns<LANES, V> at(lane, i, tile0, dim);
-        raw[i] = Vec<T, V>{};
-        if (real && at.any) raw[i] = load_vec<T, V>(row + at.first);
+// The candidates of up to 64 lanes, those that are entities first: their
+// number, and how a lane's value moves there (push) and back (pull).
+struct Packed {
+    int count, place;
+    bool real;
+    __device__ Packed(int32_t id, int32_t rows)
+    {
+        real = id >= 0 && id < rows;
+        const uint64_t mask = __ballot(real);
+        count = __popcll(mask);
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+        place = real ? before : count + (int)(threadIdx.x & 63) - before;
     }
+    __device__ int push(int x) const { return __builtin_amdgcn_ds_permute(place * 4, x); }
+    __device__ int pull(int x) const { return __builtin_amdgcn_ds_bpermute(place * 4, x); }
+};
+
+// Row of packed candidate `at` (behind the last one: of another candidate).
+template <class T, int LANES>
+__device__ __forceinline__ const T* row_of(const T* table, int64_t stride, int32_t ids, int at)
+{
+    if constexpr (LANES == 64) return table + (int64_t)__builtin_amdgcn_readlane(ids, at & 63) * stride;
+    else return table + (int64_t)__shfl(ids, at & 63) * stride;
 }
 
-// A wavefront takes up to 64 candidates (`tile`) of one query.  Its lanes
-// first read the ids, one each; then 64 / LANES rows at a time, UNROLL times
-// over before the first is used, are multiplied with the query, which stays
-// in registers, and summed over the LANES lanes.  Lane k keeps candidate k's
-// score, so that the scores leave in one store.
-template <class TE, class TQ, int LANES, int V, int NI, int UNROLL>
-__global__ __launch_bounds__(WG) void k_score(const TE* __restrict__ table, int64_t table_stride, int V_rows, int dim,
-                                              const TQ* __restrict__ queries, int64_t query_stride,
-                                              const int32_t* __restrict__ ids, int64_t id_stride,
-                                              float* __restrict__ out, int64_t out_stride, int batch, int n, int tile,
-                                              int tiles)
-{
-    constexpr int GROUPS = 64 / LANES;
-    const int lane = threadIdx.x & 63, sub = lane % LANES, group = lane / LANES;
-    const int64_t w = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
-    if (w >= (int64_t)batch * tiles) return;
-    const int64_t b = w / tiles;
-    const int k0 = (int)(w - b * tiles) * tile;
-    const int count = min(tile, n - k0);
-    int32_t id = -1;
-    if (lane < count) id = ids[b * id_stride + k0 + lane];
-    if (id >= V_rows) id = -1;
-    const bool ragged = dim % V != 0;
-    float score = 0.0f;
-    for (int tile0 = 0; tile0 < dim; tile0 += LANES * V * NI) {
-        Vec<TQ, V> q_raw[NI];
-        float q[NI][V];
-        fetch<TQ, LANES, V, NI>(queries + b * query_stride, sub, tile0, dim, true, q_raw);
-        take<TQ, LANES, V, NI>(q_raw, sub, tile0, dim, ragged, q);
-        for (int k = 0; k < count; k += GROUPS * UNROLL) {
-            Vec<TE, V> raw[UNROLL][NI];
+__device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
+
+// Sums of s[0 .. U) over the LANES lanes of each group.  Each halving of the
+// lanes halves the registers too: of two values, one goes on in the lower
+// half of the lanes, the other in the upper.
+template <int LANES, int U>
+struct Sums {
+    static constexpr int GROUPS = 64 / LANES;
+    static constexpr int R = LANES == 64 ? U / 4 : LANES == 32 ? U / 2 : U;   // registers left
+    // lane t of 16 keeps register t % R
+    static __device__ float over(float* s, int lane)
+    {
+        if constexpr (LANES == 64) {
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                const int at = k + u * GROUPS + group;
-                int32_t e;
-                if constexpr (LANES == 64) e = at < 64 ? __builtin_amdgcn_readlane(id, at & 63) : -1;
-                else e = at < 64 ? __shfl(id, at & 63) : -1;
-                fetch<TE, LANES, V, NI>(table + (int64_t)e * table_stride, sub, tile0, dim, e >= 0, raw[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                float x[NI][V], s = 0.0f;
-                take<TE, LANES, V, NI>(raw[u], sub, tile0, dim, ragged, x);
-#pragma unroll
-                for (int i = 0; i < NI; ++i)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) s = fmaf(x[i][j], q[i][j], s);
-                s = LANES == 64 ? sum64(s) : LANES == 32 ? sum32(s) : sum16(s);
-                // the sum of group g goes to lane k + u GROUPS + g
-#pragma unroll
-                for (int g = 0; g < GROUPS; ++g) {
-                    const float sg = GROUPS == 1 ? s : __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s), g * LANES));
-                    if (lane == k + u * GROUPS + g) score += sg;
-                }
+            for (int j = 0; j < U / 2; ++j) {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[j]), __float_as_uint(s[j + U / 2]), false, false);
+                s[j] = as_f(x[0]) + as_f(x[1]);
             }
         }
+        if constexpr (LANES >= 32) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(s[j]), __float_as_uint(s[j + R]), false, false);
+                s[j] = as_f(x[0]) + as_f(x[1]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) s[j] = sum16(s[j]);
+        float kept = s[0];
+#pragma unroll
+        for (int j = 1; j < R; ++j) kept = lane % R == j ? s[j] : kept;
+        return kept;
     }
-    if (lane < count) out[b * out_stride + k0 + lane] = id < 0 ? 0.0f : score;
+    // the lane that keeps the sum of value u of a group
+    static __device__ int source(int u, int group)
+    {
+        if constexpr (LANES == 64) return u / (U / 2) * 32 + u / R % 2 * 16 + u % R;
+        else if constexpr (LANES == 32) return group * 32 + u / R * 16 + u % R;
+        else return group * 16 + u;
+    }
+};
+
+// A wavefront takes `tile` (up to 64) candidates of one query.  Its lanes
+// read the ids, one each, and pack the entities; then 64 / LANES rows at a
+// time, U times over before the first is used, are multiplied with the query,
+// which stays in registers, and summed over the LANES lanes.  Lane k keeps
+// packed candidate k's score, so that the scores leave in one store.
+template <class TE, class TQ, int LANES, int V, int NI, int U>
+__global__ __launch_bounds__(64) void k_score(const TE* __restrict__ table, int64_t table_stride, int rows, int dim,
+                                              const TQ* __restrict__ queries, int64_t query_stride,
+                                              const int32_t* __restrict__ ids, int64_t id_stride,
+                                              float* __restrict__ out, int64_t out_stride, int n, int tile, int tiles)
+{
+    using Sum = Sums<LANES, U>;
+    constexpr int GROUPS = Sum::GROUPS;
+    const int lane = threadIdx.x, sub = lane % LANES, group = lane / LANES;
+    const int64_t b = blockIdx.x / tiles;
+    const int k0 = (int)(blockIdx.x - b * tiles) * tile;
+    const int count = min(tile, n - k0);
+    const int32_t id = lane < count ? ids[b * id_stride + k0 + lane] : -1;
+    const Packed packed(id, rows);
+    const int32_t all = packed.push(id);
+    const int32_t some = __builtin_amdgcn_readfirstlane(all);
+    const int32_t entity = lane < packed.count ? all : some;
+    const bool ragged = dim % V != 0;
+    float score = 0.0f;
+    if (packed.count)
+        for (int tile0 = 0; tile0 < dim; tile0 += LANES * V * NI) {
+            const TQ* query = queries + b * query_stride;
+            Vec<TQ, V> q_raw[1][NI];
+            float q[NI][V];
+            fetch<TQ, LANES, V, NI, 1>(&query, sub, tile0, dim, q_raw);
+            take<TQ, LANES, V, NI>(q_raw[0], sub, tile0, dim, ragged, q);
+            for (int k = 0; k < packed.count; k += GROUPS * U) {
+                Vec<TE, V> raw[U][NI];
+                const TE* row[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) row[u] = row_of<TE, LANES>(table, table_stride, entity, k + u * GROUPS + group);
+                fetch<TE, LANES, V, NI, U>(row, sub, tile0, dim, raw);
+                float s[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float x[NI][V];
+                    s[u] = 0.0f;
+                    take<TE, LANES, V, NI>(raw[u], sub, tile0, dim, ragged, x);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) s[u] = fmaf(x[i][j], q[i][j], s[u]);
+                }
+                const float kept = Sum::over(s, lane);
+                const int at = lane - k;
+                const float mine = __int_as_float(__builtin_amdgcn_ds_bpermute(
+                    Sum::source(at / GROUPS % U, at % GROUPS) * 4, __float_as_int(kept)));
+                if (at >= 0 && at < GROUPS * U) score += mine;
+            }
+        }
+    const float back = __int_as_float(packed.pull(__float_as_int(score)));
+    if (lane < count) out[b * out_stride + k0 + lane] = packed.real ? back : 0.0f;
 }
 
 // A workgroup takes one query's candidates [k0, k1) for LANES x V x NI of
 // its columns; its wavefronts deal the candidates out 64 at a time and add
 // their sums in LDS.  Several workgroups that share a query (splits > 1:
 // few queries with long lists) write partial sums, which k_join adds.
-template <class TE, class TO, int LANES, int V, int NI, int UNROLL>
-__global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table, int64_t table_stride, int V_rows, int dim,
+template <class TE, class TO, int LANES, int V, int NI, int U>
+__global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table, int64_t table_stride, int rows, int dim,
                                                    const int32_t* __restrict__ ids, int64_t id_stride,
                                                    const float* __restrict__ grad, int64_t grad_stride,
                                                    TO* __restrict__ out, int64_t out_stride, int n, int span, int splits,
@@ -144,40 +216,44 @@ __global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table,
     const int tile0 = blockIdx.y * WIDTH;
     const bool ragged = dim % V != 0;
     float acc[NI][V] = {};
-    for (int base = k0 + wave * 64; base < k1; base += WAVES * 64) {
-        const int count = min(64, k1 - base);
+    // equal shares of at most 64 candidates
+    const int rounds = (k1 - k0 + 64 * WAVES - 1) / (64 * WAVES);
+    const int step = (k1 - k0 + WAVES * rounds - 1) / max(WAVES * rounds, 1);
+    for (int base = k0 + wave * step; base < k1; base += WAVES * step) {
+        const int count = min(step, k1 - base);
         int32_t id = -1;
         float g = 0.0f;
         if (lane < count) {
             id = ids[b * id_stride + base + lane];
             g = grad[b * grad_stride + base + lane];
         }
-        if (id >= V_rows) id = -1;
-        for (int k = 0; k < count; k += GROUPS * UNROLL) {
-            Vec<TE, V> raw[UNROLL][NI];
-            float w[UNROLL];
+        const Packed packed(id, rows);
+        const int32_t all = packed.push(id);
+        const float weight = __int_as_float(packed.push(__float_as_int(g)));
+        const int32_t some = __builtin_amdgcn_readfirstlane(all);
+        const int32_t entity = lane < packed.count ? all : some;
+        for (int k = 0; k < packed.count; k += GROUPS * U) {
+            Vec<TE, V> raw[U][NI];
+            const TE* row[U];
+            float w[U];
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const int at = k + u * GROUPS + group;
-                int32_t e;
-                if constexpr (LANES == 64) {
-                    e = at < 64 ? __builtin_amdgcn_readlane(id, at & 63) : -1;
-                    w[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), at & 63));
-                } else {
-                    e = at < 64 ? __shfl(id, at & 63) : -1;
-                    w[u] = __shfl(g, at & 63);
-                }
-                if (e < 0) w[u] = 0.0f;
-                fetch<TE, LANES, V, NI>(table + (int64_t)e * table_stride, sub, tile0, dim, e >= 0, raw[u]);
+                row[u] = row_of<TE, LANES>(table, table_stride, entity, at);
+                if constexpr (LANES == 64) w[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), at & 63));
+                else w[u] = __shfl(weight, at & 63);
             }
+            fetch<TE, LANES, V, NI, U>(row, sub, tile0, dim, raw);
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
+            for (int u = 0; u < U; ++u) {
                 float x[NI][V];
                 take<TE, LANES, V, NI>(raw[u], sub, tile0, dim, ragged, x);
+                if (k + u * GROUPS + group < packed.count) {
 #pragma unroll
-                for (int i = 0; i < NI; ++i)
+                    for (int i = 0; i < NI; ++i)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) acc[i][j] = fmaf(w[u], x[i][j], acc[i][j]);
+                        for (int j = 0; j < V; ++j) acc[i][j] = fmaf(w[u], x[i][j], acc[i][j]);
+                }
             }
         }
     }
@@ -204,30 +280,41 @@ __global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table,
     }
 }
 
+// 64 columns of a query: 16 wavefronts add every 16th partial sum each.
 template <class TO>
-__global__ __launch_bounds__(WG) void k_join(const float* __restrict__ partial, int splits, int dim, TO* __restrict__ out,
-                                             int64_t out_stride, int64_t total)
+__global__ __launch_bounds__(1024) void k_join(const float* __restrict__ partial, int splits, int dim, TO* __restrict__ out,
+                                               int64_t out_stride)
 {
-    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x;
-    if (t >= total) return;
-    const int64_t b = t / dim, c = t - b * dim;
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t b = blockIdx.x;
+    const int c = blockIdx.y * 64 + lane;
     float s = 0.0f;
-    for (int k = 0; k < splits; ++k) s += partial[(b * splits + k) * dim + c];
-    out[b * out_stride + c] = (TO)s;
+    if (c < dim) {
+#pragma unroll 4
+        for (int k = wave; k < splits; k += 16) s += partial[(b * splits + k) * dim + c];
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < dim) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += part[w][lane];
+        out[b * out_stride + c] = (TO)s;
+    }
 }
 
 template <class TE, class TQ, int LANES, int V, int NI, int UNROLL>
 int score_as(const smore_score_args& a, const void* table, const void* queries, const int32_t* ids, float* scores,
              hipStream_t st, const char** err)
 {
-    // candidates per wavefront: 64, fewer where that leaves CUs without work
+    // candidates per wavefront: up to 64, fewer where that leaves CUs without work
     int tile = 64;
     while (tile > 8 && (int64_t)a.batch * ((a.n + tile - 1) / tile) < 4096) tile /= 2;
     const int tiles = (a.n + tile - 1) / tile;
-    const int64_t blocks = ((int64_t)a.batch * tiles + WAVES - 1) / WAVES;
-    k_score<TE, TQ, LANES, V, NI, UNROLL><<<(unsigned)blocks, WG, 0, st>>>(
+    tile = (a.n + tiles - 1) / tiles;
+    k_score<TE, TQ, LANES, V, NI, UNROLL><<<(unsigned)((int64_t)a.batch * tiles), 64, 0, st>>>(
         (const TE*)table, a.table_stride, a.n_rows, a.dim, (const TQ*)queries, a.query_stride, ids, a.candidate_stride,
-        scores, a.score_stride, a.batch, a.n, tile, tiles);
+        scores, a.score_stride, a.n, tile, tiles);
     return launched(err);
 }
 
@@ -236,19 +323,19 @@ int score_typed(const smore_score_args& a, const void* table, const void* querie
                 hipStream_t st, const char** err)
 {
     constexpr int V = 16 / sizeof(TE);
-    if (a.dim < V) return score_as<TE, TQ, 16, 1, 1, 4>(a, table, queries, ids, scores, st, err);
-    if (a.dim <= 16 * V) return score_as<TE, TQ, 16, V, 1, 4>(a, table, queries, ids, scores, st, err);
+    if (a.dim < V) return score_as<TE, TQ, 16, 1, 1, 8>(a, table, queries, ids, scores, st, err);
+    if (a.dim <= 16 * V) return score_as<TE, TQ, 16, V, 1, 8>(a, table, queries, ids, scores, st, err);
     if (a.dim <= 32 * V) return score_as<TE, TQ, 32, V, 1, 8>(a, table, queries, ids, scores, st, err);
     if (a.dim <= 64 * V) return score_as<TE, TQ, 64, V, 1, 8>(a, table, queries, ids, scores, st, err);
     return score_as<TE, TQ, 64, V, 2, 4>(a, table, queries, ids, scores, st, err);
 }
 
 // Workgroups that share a query: enough to fill the chip, each wavefront
-// with at least 8 candidates.
+// with at least 16 candidates.
 void grad_split(const smore_score_args& a, int* splits, int* span)
 {
     int64_t s = 1;
-    while ((int64_t)a.batch * s < 2048 && a.n > s * WAVES * 8) s *= 2;
+    while ((int64_t)a.batch * s < 512 && a.n > s * WAVES * 16) s *= 2;
     *span = (int)((a.n + s - 1) / s);
     *splits = *span > 0 ? (a.n + *span - 1) / *span : 1;
 }
@@ -264,9 +351,8 @@ int grad_as(const smore_score_args& a, const void* table, const int32_t* ids, co
         (const TE*)table, a.table_stride, a.n_rows, a.dim, ids, a.candidate_stride, grad, a.score_stride, (TO*)out,
         a.query_stride, a.n, span, splits, (float*)ws);
     if (splits > 1) {
-        const int64_t total = (int64_t)a.batch * a.dim;
-        k_join<TO><<<(unsigned)((total + WG - 1) / WG), WG, 0, st>>>((const float*)ws, splits, a.dim, (TO*)out, a.query_stride,
-                                                                     total);
+        k_join<TO><<<dim3((unsigned)a.batch, (unsigned)((a.dim + 63) / 64)), 1024, 0, st>>>((const float*)ws, splits, a.dim,
+                                                                                           (TO*)out, a.query_stride);
     }
     return launched(err);
 }
@@ -276,8 +362,8 @@ int grad_typed(const smore_score_args& a, const void* table, const int32_t* ids,
                hipStream_t st, const char** err)
 {
     constexpr int V = 16 / sizeof(TE);
-    if (a.dim < V) return grad_as<TE, TO, 16, 1, 1, 4>(a, table, ids, grad, out, ws, st, err);
-    if (a.dim <= 16 * V) return grad_as<TE, TO, 16, V, 1, 4>(a, table, ids, grad, out, ws, st, err);
+    if (a.dim < V) return grad_as<TE, TO, 16, 1, 1, 8>(a, table, ids, grad, out, ws, st, err);
+    if (a.dim <= 16 * V) return grad_as<TE, TO, 16, V, 1, 8>(a, table, ids, grad, out, ws, st, err);
     if (a.dim <= 32 * V) return grad_as<TE, TO, 32, V, 1, 8>(a, table, ids, grad, out, ws, st, err);
     if (a.dim <= 64 * V) return grad_as<TE, TO, 64, V, 1, 8>(a, table, ids, grad, out, ws, st, err);
     return grad_as<TE, TO, 64, V, 2, 4>(a, table, ids, grad, out, ws, st, err);
