@@ -533,15 +533,15 @@ def _launch(device, stream, call):
         with torch.cuda.stream(stream):
             return call(stream.cuda_stream)
     if torch.cuda.current_device() == device.index:
-        return call(torch.cuda.current_stream().cuda_stream)
+        return call(torch._C._cuda_getCurrentRawStream(device.index))
     with torch.cuda.device(device):
-        return call(torch.cuda.current_stream(device).cuda_stream)
+        return call(torch._C._cuda_getCurrentRawStream(device.index))
 
 
-def _fits(t, shape, dtype, device) -> bool:
-    """A tensor of this shape, type and device whose rows are contiguous (the
-    distance of two rows is free)."""
-    return t.shape == shape and t.dtype == dtype and t.device == device and \
+def _fits(t, shape, dtype, index: int) -> bool:
+    """A tensor of this shape and type on this GPU whose rows are contiguous
+    (the distance of two rows is free)."""
+    return t.shape == shape and t.dtype is dtype and t.get_device() == index and \
         (len(shape) < 2 or shape[1] < 2 or t.stride(1) == 1)
 
 
@@ -574,11 +574,12 @@ def _score_args(table, candidates, other, other_name: str, grad_scores, grad_nam
     v, dim = table.shape
     shape = candidates.shape
     batch, n = shape
-    device, te, tq = table.device, table.dtype, other.dtype
+    index, te, tq = table.get_device(), table.dtype, other.dtype
     wide = (torch.float32, torch.bfloat16)
-    if not (te in wide and tq in wide and _fits(table, table.shape, te, device)
-            and _fits(candidates, shape, torch.int32, device) and _fits(other, (batch, dim), tq, device)
-            and _fits(grad_scores, shape, torch.float32, device)):
+    if not (te in wide and tq in wide and _fits(table, table.shape, te, index)
+            and _fits(candidates, shape, torch.int32, index) and _fits(other, (batch, dim), tq, index)
+            and _fits(grad_scores, shape, torch.float32, index)):
+        device = table.device
         _operand("table", table, table.shape, wide, device)
         _operand("candidates", candidates, shape, (torch.int32,), device)
         _operand(other_name, other, (batch, dim), wide, device)
@@ -677,14 +678,14 @@ def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_
     scale = 1.0
     if weight is not None and not isinstance(weight, torch.Tensor):
         scale, weight = float(weight), None
-    row, i32, f32 = (batch,), torch.int32, torch.float32
-    good = dtype in _TYPES and _fits(positive, row, dtype, device) and (n < 2 or negatives.stride(1) == 1) \
-        and (ref_positive is None or (_fits(ref_positive, row, dtype, device) and _fits(ref_negatives, shape, dtype, device))) \
-        and (n_valid is None or (_fits(n_valid, row, i32, device) and n_valid.is_contiguous())) \
-        and (mask is None or (_fits(mask, (batch, (n + 31) // 32), i32, device) and mask.is_contiguous())) \
-        and (weight is None or (_fits(weight, row, f32, device) and weight.is_contiguous())) \
-        and (loss is None or (_fits(loss, row, f32, device) and loss.is_contiguous())) \
-        and (grad_p is None or (_fits(grad_p, row, dtype, device) and _fits(grad_n, shape, dtype, device)))
+    row, i32, f32, at = (batch,), torch.int32, torch.float32, negatives.get_device()
+    good = dtype in _TYPES and _fits(positive, row, dtype, at) and (n < 2 or negatives.stride(1) == 1) \
+        and (ref_positive is None or (_fits(ref_positive, row, dtype, at) and _fits(ref_negatives, shape, dtype, at))) \
+        and (n_valid is None or (_fits(n_valid, row, i32, at) and n_valid.is_contiguous())) \
+        and (mask is None or (_fits(mask, (batch, (n + 31) // 32), i32, at) and mask.is_contiguous())) \
+        and (weight is None or (_fits(weight, row, f32, at) and weight.is_contiguous())) \
+        and (loss is None or (_fits(loss, row, f32, at) and loss.is_contiguous())) \
+        and (grad_p is None or (_fits(grad_p, row, dtype, at) and _fits(grad_n, shape, dtype, at)))
     if not good:
         _check_preference(batch, n, dtype, device,
                           {"positive": positive, "negatives": negatives, "ref_positive": ref_positive,
@@ -813,7 +814,8 @@ class AdamW:
         # whether scales allow steps by rows and of the whole, and its last gradient's type
         n = len(self.params)
         self._list = (AdamWTensor * n)()
-        self._seen, self._by_rows, self._whole, self._last = [None] * n, [True] * n, [True] * n, [None] * n
+        self._items = [self._list[k] for k in range(n)]
+        self._seen, self._by_rows, self._whole, self._last, self._empty = ([None] * n for _ in range(5))
         for k in range(n):
             self._describe(k)
 
@@ -845,13 +847,13 @@ class AdamW:
                     (numel is not None and t.numel() != numel) or (numel is None and tuple(t.shape) != tuple(shapes[name])):
                 raise ValueError(f"{name} of parameter {k} must be a contiguous {dtype} tensor on {self.device} that "
                                  f"fits {tuple(p.shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        x = self._list[k]
+        x = self._items[k]
         x.param, x.m, x.v = p.data_ptr(), state["m"].data_ptr(), state["v"].data_ptr()
         x.m_scale, x.v_scale = (state["m_scale"].data_ptr(), state["v_scale"].data_ptr()) if self.bits == 8 else (None, None)
         x.n_rows, x.dim = (p.shape[0], p.shape[1]) if p.dim() == 2 else (1, p.numel())
         x.param_type, x.bits, x.index, x.weight_decay = _TYPES[p.dtype], self.bits, k, self.weight_decay[k]
         self._seen[k] = [p.shape, p] + [t.data_ptr() for t in (p, *(state[n] for n in shapes))]
-        self._by_rows[k], self._whole[k], self._last[k] = by_rows, whole, None
+        self._by_rows[k], self._whole[k], self._last[k], self._empty[k] = by_rows, whole, None, p.numel() == 0
 
     def step(self, grads, grad_scale=None, stream=None) -> None:
         """One step.  grads: for each parameter a contiguous tensor of its
@@ -863,7 +865,7 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        used, device, scaled = [], self.device, self.bits == 8
+        used, device, scaled, tables = [], self.device, self.bits == 8, False
         for k, g in enumerate(grads):
             if g is None:
                 continue
@@ -875,19 +877,20 @@ class AdamW:
                                                                         or state["v_scale"].data_ptr() != seen[6])):
                 self._describe(k)
             if type(g) is RowGrad:
-                self._rows(k, self._list[k], p, g)
+                self._rows(k, self._items[k], p, g)
+                tables = True
             else:
                 if g.shape != shape or g.dtype not in _TYPES or g.device != device or not g.is_contiguous():
                     raise ValueError(f"gradient {k} must be a contiguous tensor of shape {tuple(shape)} on {device}, "
                                      f"got {g.dtype} {tuple(g.shape)} on {g.device}")
-                x = self._list[k]
+                x = self._items[k]
                 x.grad = g.data_ptr()
                 if self._last[k] is not g.dtype:
                     if not self._whole[k]:
                         raise ValueError(f"the moments of parameter {k} have scales per row: its gradient must be a RowGrad")
                     x.grad_type, x.rows, x.order, x.coef = _TYPES[g.dtype], None, None, None
                     self._last[k] = g.dtype
-                if not shape.numel():
+                if self._empty[k]:
                     continue
             used.append(k)
         for name, t, dtype in (("lr", self.lr if isinstance(self.lr, torch.Tensor) else None, torch.float32),
@@ -903,7 +906,7 @@ class AdamW:
                          _ptr(self.device_steps), self.lr.data_ptr() if device_lr else None, _ptr(grad_scale),
                          0 if self.seed is None else self.seed, 0 if self.seed is None else ADAMW_STOCHASTIC)
         L, n, need = lib(), len(used), 0
-        if any(type(grads[k]) is RowGrad for k in used):
+        if tables:
             size = ctypes.c_size_t()
             _check(L.smore_adamw_workspace_bytes(ts, n, ctypes.byref(size)))
             need = size.value
@@ -921,7 +924,7 @@ class AdamW:
         _check(_launch(device, stream, call))
         self.steps += 1
         # autograd sees that they changed
-        torch.autograd.graph.increment_version([self.params[k] for k in used if not self.params[k].is_inference()])
+        torch.autograd.graph.increment_version([p for p in (self.params[k] for k in used) if not p.is_inference()])
 
     def _rows(self, k: int, x, p, g: RowGrad) -> None:
         torch = _torch

@@ -36,6 +36,7 @@ constexpr int PER = 8;                  // consecutive elements of a lane
 constexpr int CHUNK = 64 * PER;         // elements of a wavefront: four blocks of 128
 constexpr int BLOCK = SMORE_ADAMW_BLOCK;
 constexpr int RUN = 128;                // entries whose sum is made ahead in long runs
+constexpr int AHEAD = 4;                // vectors of a run in flight
 
 // One step's constants.
 struct Step {
@@ -457,13 +458,20 @@ __device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, 
     for (int64_t at = first; at < end; at += 64) {
         const int n = (int)min((int64_t)64, end - at);
         const Entry e = entry_of(r, at + lane, end);
-        for (int i = 0; i < n; ++i) {
-            const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, i);
-            const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i));
-            float x[PER];
-            load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x);
+        for (int i = 0; i < n; i += AHEAD) {
+            float x[AHEAD][PER];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[j]);
+            for (int q = 0; q < AHEAD; ++q) {
+                const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, min(i + q, n - 1));
+                load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                if (i + q >= n) break;
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i + q));
+#pragma unroll
+                for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[q][j]);
+            }
         }
     }
 }
@@ -488,13 +496,13 @@ __global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, double* __r
     }
 }
 
-// A wavefront per entry; the first entry of a row's run takes the row.
+// A wavefront per entry, each a workgroup of its own; the first entry of a
+// row's run takes the row, the others end at once and leave their place.
 template <class TP, class TG, int BITS>
-__global__ __launch_bounds__(WG) void k_adamw_rows(const RowsTensor r, const Hyper hyper)
+__global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t i = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * WAVES + (threadIdx.x >> 6)));
-    if (i >= r.n_entries) return;
+    const int lane = threadIdx.x;
+    const int64_t i = blockIdx.x;
     const int32_t row = r.rows[i];
     if (row < 0 || row >= r.n_rows || (i > 0 && r.rows[i - 1] == row)) return;
     Step s;
@@ -613,7 +621,7 @@ int rows_as(const smore_adamw_tensor& x, const Hyper& h, double* partial, hipStr
     r.per_inverse = 1.0 / r.per;
     const int64_t sums = x.n_entries / RUN;
     if (sums) k_run_sums<TG><<<(unsigned)((sums + WAVES - 1) / WAVES), WG, 0, st>>>(r, partial);
-    if (x.n_entries) k_adamw_rows<TP, TG, BITS><<<(unsigned)((x.n_entries + WAVES - 1) / WAVES), WG, 0, st>>>(r, h);
+    if (x.n_entries) k_adamw_rows<TP, TG, BITS><<<(unsigned)x.n_entries, 64, 0, st>>>(r, h);
     return launched(err);
 }
 

@@ -36,14 +36,11 @@ struct LossRow {
     float beta, eps, scale;
 };
 
-// log(1 + e), e in [0, 1]: the logarithm of the rounded 1 + e, corrected by
-// the ratio of e to what 1 + e kept of it
-__device__ __forceinline__ float log_1p(float e)
-{
-    const float u = 1.0f + e;
-    const float l = __logf(u) * (e * __builtin_amdgcn_rcpf(u - 1.0f));
-    return u == 1.0f ? e : l;
-}
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+
+// All ones where bit j of the valid places is set, else 0.
+__device__ __forceinline__ uint32_t ones(uint32_t ok, int j) { return (uint32_t)((int32_t)(ok << (31 - j)) >> 31); }
+__device__ __forceinline__ float keep(uint32_t ok, int j, float x) { return __uint_as_float(__float_as_uint(x) & ones(ok, j)); }
 
 // Sum over the WAVES wavefronts of a row of a value that every lane of a
 // wavefront has.
@@ -93,19 +90,22 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
     if (REF) base -= (float)((const T*)a.ref_pos)[b * a.ref_pos_stride];
     const float gain = GRAD ? a.beta * a.scale * (a.weight ? a.weight[b] : 1.0f) : 0.0f;
 
-    float z[STEPS][V];
+    // d = the log ratio of a negative over the positive's; z = -beta d
+    float d[STEPS][V];
     uint32_t ok[STEPS];   // bit j: score j of the block is valid
+    bool full;            // every place of the wavefront's blocks is
     auto fetch = [&](int at0) {
         float x[STEPS][V], r[STEPS][V];
+        uint32_t both = (1u << V) - 1u;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const int k = at0 + s * BLOCK + my;
             ok[s] = 0;
             if (k < limit) {
-                const int have = min(V, limit - k);
-                ok[s] = (1u << have) - 1u;
+                ok[s] = (1u << min(V, limit - k)) - 1u;
                 if (bits) ok[s] &= bits[k >> 5] >> (k & 31);
             }
+            both &= ok[s];
 #pragma unroll
             for (int j = 0; j < V; ++j) x[s][j] = r[s][j] = 0.0f;
             if (ok[s]) {
@@ -113,34 +113,46 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
                 if (REF) load_floats<T, V>(ref + k, a.n - k, r[s]);
             }
         }
+        full = __all(both == (1u << V) - 1u);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-            for (int j = 0; j < V; ++j) z[s][j] = a.beta * (base - (REF ? x[s][j] - r[s][j] : x[s][j]));
+            for (int j = 0; j < V; ++j) d[s][j] = (REF ? x[s][j] - r[s][j] : x[s][j]) - base;
     };
     T* grad = GRAD ? (T*)a.grad_neg + b * a.grad_neg_stride : nullptr;
 
     if constexpr (!SOFTMAX) {
         float loss = 0.0f, slopes = 0.0f;
+        const float unit = share * gain;
         for (int at0 = 0; at0 < a.n; at0 += SPAN) {
             fetch(at0);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 const int k = at0 + s * BLOCK + my;
-                float g[V];
+                float l[V], g[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float e = __expf(-fabsf(z[s][j]));
-                    float l = fmaxf(-z[s][j], 0.0f);
-                    if (a.eps != 0.0f) l = fmaf(a.eps, fmaxf(z[s][j], 0.0f), (1.0f - a.eps) * l);
-                    l += log_1p(e);
-                    const bool on = (ok[s] >> j) & 1;
-                    loss += on ? l : 0.0f;
-                    if (GRAD) {
-                        const float sigma = (z[s][j] >= 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);   // sigma(-z)
-                        g[j] = on ? (sigma - a.eps) * share * gain : 0.0f;
-                        slopes -= g[j];
+                    const float y = a.beta * d[s][j];                                  // -z
+                    const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(y));         // exp(-|z|)
+                    const float u = 1.0f + e, r = __builtin_amdgcn_rcpf(u);
+                    // log(1 + e): the logarithm of u and what u lost of e
+                    const float tail = fmaf(__builtin_amdgcn_logf(u), LN2, (e - (u - 1.0f)) * r);
+                    l[j] = fmaxf(y, 0.0f);
+                    if (a.eps != 0.0f) l[j] = fmaf(a.eps, fmaxf(-y, 0.0f), (1.0f - a.eps) * l[j]);
+                    l[j] += tail;
+                    if (GRAD) g[j] = ((y <= 0.0f ? e : 1.0f) * r - a.eps) * unit;     // sigma(-z)
+                }
+                if (!full) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        l[j] = keep(ok[s], j, l[j]);
+                        if (GRAD) g[j] = keep(ok[s], j, g[j]);
                     }
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    loss += l[j];
+                    if (GRAD) slopes -= g[j];
                 }
                 if (GRAD && k < a.n) store_floats<T, V>(grad + k, a.n - k, g);
             }
@@ -152,51 +164,72 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
             if (GRAD) ((T*)a.grad_pos)[b * a.grad_pos_stride] = (T)slopes;
         }
     } else {
-        // running maximum (of 0, the positive's own term, on) and sum of each lane
+        // exponents to the base 2; running maximum (of 0, the positive's own
+        // term, on) and sum of each lane
+        const float rate = a.beta * LOG2E;
         float top = 0.0f, sum = 0.0f;
         float e[STEPS][V];
-        for (int at0 = 0; at0 < a.n; at0 += SPAN) {
+        auto exponents = [&](int at0) {
             fetch(at0);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int j = 0; j < V; ++j) e[s][j] = rate * d[s][j];
+            if (!full) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const uint32_t m = ones(ok[s], j);
+                        e[s][j] = __uint_as_float((__float_as_uint(e[s][j]) & m) | (0xFF800000u & ~m));   // or -infinity
+                    }
+            }
+        };
+        for (int at0 = 0; at0 < a.n; at0 += SPAN) {
+            exponents(at0);
             float m = top;
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if ((ok[s] >> j) & 1) m = fmaxf(m, -z[s][j]);
-            sum *= __expf(top - m);
+                for (int j = 0; j < V; ++j) m = fmaxf(m, e[s][j]);
+            sum *= __builtin_amdgcn_exp2f(top - m);
             top = m;
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    e[s][j] = (ok[s] >> j) & 1 ? __expf(-z[s][j] - top) : 0.0f;
+                    e[s][j] = __builtin_amdgcn_exp2f(e[s][j] - top);
                     sum += e[s][j];
                 }
         }
         float high = across<WAVES>(max64(top), lds, wave, [](float x, float y) { return fmaxf(x, y); });
-        const float mine = __expf(top - high);
+        const float mine = __builtin_amdgcn_exp2f(top - high);
         sum = across<WAVES>(sum64(sum * mine), lds, wave, [](float x, float y) { return x + y; });
-        const float total = __expf(-high) + sum;
+        const float total = __builtin_amdgcn_exp2f(-high) + sum;
         if (lane == 0 && wave == 0) {
-            if (a.loss) a.loss[b] = high > 0.0f ? high + __logf(total) : log1pf(sum);
+            if (a.loss) a.loss[b] = high > 0.0f ? fmaf(high, LN2, __logf(total)) : log1pf(sum);
             if (GRAD) ((T*)a.grad_pos)[b * a.grad_pos_stride] = (T)(sum == 0.0f ? 0.0f : -gain * (sum / total));
         }
         if constexpr (GRAD) {
-            const float unit = gain / total;
+            const float unit = mine * (gain / total);
             for (int at0 = 0; at0 < a.n; at0 += SPAN) {
                 if (a.n > SPAN) {
-                    fetch(at0);
+                    exponents(at0);
 #pragma unroll
                     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                        for (int j = 0; j < V; ++j) e[s][j] = (ok[s] >> j) & 1 ? __expf(-z[s][j] - top) : 0.0f;
+                        for (int j = 0; j < V; ++j) e[s][j] = __builtin_amdgcn_exp2f(e[s][j] - top);
                 }
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
                     const int k = at0 + s * BLOCK + my;
                     float g[V];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) g[j] = (ok[s] >> j) & 1 ? e[s][j] * mine * unit : 0.0f;
+                    for (int j = 0; j < V; ++j) g[j] = e[s][j] * unit;
+                    if (!full) {      // a unit that is not finite stays out of places that are not valid
+#pragma unroll
+                        for (int j = 0; j < V; ++j) g[j] = keep(ok[s], j, g[j]);
+                    }
                     if (k < a.n) store_floats<T, V>(grad + k, a.n - k, g);
                 }
             }

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table,
     float acc[NI][V] = {};
     // equal shares of at most 64 candidates
     const int rounds = (k1 - k0 + 64 * WAVES - 1) / (64 * WAVES);
-    const int step = (k1 - k0 + WAVES * rounds - 1) / max(WAVES * rounds, 1);
+    const int step = max(1, (k1 - k0 + WAVES * rounds - 1) / max(1, WAVES * rounds));
     for (int base = k0 + wave * step; base < k1; base += WAVES * step) {
         const int count = min(step, k1 - base);
         int32_t id = -1;
@@ -327,7 +327,7 @@ int score_typed(const smore_score_args& a, const void* table, const void* querie
     if (a.dim <= 16 * V) return score_as<TE, TQ, 16, V, 1, 8>(a, table, queries, ids, scores, st, err);
     if (a.dim <= 32 * V) return score_as<TE, TQ, 32, V, 1, 8>(a, table, queries, ids, scores, st, err);
     if (a.dim <= 64 * V) return score_as<TE, TQ, 64, V, 1, 8>(a, table, queries, ids, scores, st, err);
-    return score_as<TE, TQ, 64, V, 2, 4>(a, table, queries, ids, scores, st, err);
+    return score_as<TE, TQ, 64, V, 2, 8>(a, table, queries, ids, scores, st, err);
 }
 
 // Workgroups that share a query: enough to fill the chip, each wavefront
@@ -366,7 +366,7 @@ int grad_typed(const smore_score_args& a, const void* table, const int32_t* ids,
     if (a.dim <= 16 * V) return grad_as<TE, TO, 16, V, 1, 8>(a, table, ids, grad, out, ws, st, err);
     if (a.dim <= 32 * V) return grad_as<TE, TO, 32, V, 1, 8>(a, table, ids, grad, out, ws, st, err);
     if (a.dim <= 64 * V) return grad_as<TE, TO, 64, V, 1, 8>(a, table, ids, grad, out, ws, st, err);
-    return grad_as<TE, TO, 64, V, 2, 4>(a, table, ids, grad, out, ws, st, err);
+    return grad_as<TE, TO, 64, V, 2, 8>(a, table, ids, grad, out, ws, st, err);
 }
 
 }  // namespace
