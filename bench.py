@@ -327,6 +327,85 @@ def verify_bench(cfg, g, types, steps, warmup, stream):
                           "complete_queries": int((nv == n_cand).sum().item())}), flush=True)
 
 
+def train_bench(cfg, g, types, steps, warmup, stream, dim):
+    """A training step on each sampled batch of the workload: sample, scores of
+    the positives and negatives, the preference loss (softmax) and its
+    gradients, and AdamW on the candidates' rows of the entity table and on
+    the relation table.  The entity table is bf16 with moments in 8 bits, the
+    relation table fp32; a query's vector is its first anchor's row times its
+    relations' rows (the anchors' rows are read, not stepped).  One JSON line
+    per shape, with the time of each part."""
+    import torch
+
+    import paper_2110_14890_amd as sm
+
+    dev = torch.device("cuda")
+    gen = torch.Generator(device="cuda").manual_seed(cfg.seed)
+    table = torch.empty((g.V, dim), dtype=torch.bfloat16, device=dev)
+    for part in table.split(1 << 20):
+        part.copy_(torch.randn(part.shape, generator=gen, device=dev).mul_(0.05))
+    relations = torch.randn((g.R, dim), generator=gen, device=dev)
+    entities = sm.AdamW([table], lr=1e-3, bits=8, seed=cfg.seed, tables=(0,))
+    operators = sm.AdamW([relations], lr=1e-3)
+    per = cfg.n_neg + 1
+    parts = ("sample", "queries", "score", "loss", "grad", "rows", "relations")
+    for qt in types:
+        dag = sm.query_preset(qt)
+        out = sm.alloc_outputs(cfg.batch, cfg.n_neg)
+        ws = sm.Workspace()
+
+        def step(k, mark):
+            args = sm.make_args(cfg.batch, cfg.n_neg, seed=cfg.seed, query_offset=k * cfg.batch)
+            sm.sample_into(g, dag, args, out, workspace=ws)
+            mark("sample")
+            ids = torch.cat([out["positive"][:, None], out["negatives"]], 1)
+            leaf = relations.detach().requires_grad_()
+            used = (out["relations"] >= 0)[:, :, None]
+            rel = torch.where(used, leaf[out["relations"].clamp(min=0).long()], 1.0).prod(1)
+            queries = table[out["anchors"][:, 0].clamp(min=0).long()].float() * rel
+            mark("queries")
+            scores = sm.score(table, queries.detach(), ids)
+            mark("score")
+            coef = torch.empty_like(scores)
+            loss = torch.empty(cfg.batch, device=dev)
+            sm.preference_loss_into(scores[:, 0], scores[:, 1:],
+                                    {"loss": loss, "grad_positive": coef[:, 0], "grad_negatives": coef[:, 1:]},
+                                    n_valid=out["n_valid"], kind="softmax", beta=1.0, weight=1.0 / cfg.batch)
+            mark("loss")
+            grad = sm.score_grad(table, ids, coef)
+            mark("grad")
+            entities.step([sm.row_grad(ids, queries.detach(), coef=coef, per=per)])
+            mark("rows")
+            queries.backward(grad)
+            operators.step([leaf.grad])
+            mark("relations")
+            return loss
+
+        with torch.cuda.stream(stream):
+            for k in range(warmup):
+                step(k, lambda name: None)
+            torch.cuda.synchronize()
+            total = dict.fromkeys(parts, 0.0)
+            t0 = time.perf_counter()
+            for k in range(steps):
+                events = [torch.cuda.Event(enable_timing=True)]
+                events[0].record(stream)
+
+                def mark(name):
+                    events.append(torch.cuda.Event(enable_timing=True))
+                    events[-1].record(stream)
+
+                loss = step(warmup + k, mark)
+                torch.cuda.synchronize()
+                for name, a, b in zip(parts, events, events[1:]):
+                    total[name] += a.elapsed_time(b) / steps
+            ms = (time.perf_counter() - t0) / steps * 1e3
+        print(json.dumps({"mode": "training", "shape": qt, "queries": cfg.batch, "negatives": cfg.n_neg, "dim": dim,
+                          "ms_per_step": round(ms, 3), "queries_per_s": round(cfg.batch / ms * 1e3, 1),
+                          "ms": {k: round(v, 3) for k, v in total.items()},
+                          "mean_loss": round(loss[out["n_valid"] > 0].mean().item(), 4)}), flush=True)
+
+
 def cpu_baseline(cfg, og, types, seconds, threads, visible):
     """The CPU oracle, timed on the host on the first queries of each shape
     (a bounded sample of the same workload), on every CPU the job has.  A
@@ -568,6 +647,10 @@ def main():
     ap.add_argument("--verify", action="store_true",
                     help="instead of the benchmark: evaluation-time verification of 1,000 "
                          "candidates per query, and 1,000 filtered negatives per query")
+    ap.add_argument("--train", action="store_true",
+                    help="instead of the benchmark: training steps on sampled batches (scores, "
+                         "preference loss, AdamW on the candidates' rows)")
+    ap.add_argument("--dim", type=int, default=400, help="width of the tables of --train")
     ap.add_argument("--c-sweep", action="store_true",
                     help="instead of the benchmark: minibatch time vs max expansion C, "
                          "GPU vs the exhaustive CPU oracle (2p, ip, pni)")
@@ -664,6 +747,9 @@ def main():
         return
     if args.verify:
         verify_bench(cfg, g, types, args.steps, args.warmup, stream)
+        return
+    if args.train:
+        train_bench(cfg, g, types, args.steps, args.warmup, stream, args.dim)
         return
     neg_tries = 4 * cfg.n_neg
     dags = {qt: sm.query_preset(qt) for qt in types}

@@ -466,8 +466,8 @@ int smore_preference_loss(const smore_preference_args *args, const smore_prefere
    consecutive elements of a row (a dense tensor is one row): m_scale,
    v_scale fp32, [ceil(elements / block)], for tables [n_rows,
    ceil(dim / block)].  Moments that are all zero bytes are moments 0, a block
-   whose moments are all below 2^-100 is held as 0, and one with a moment that
-   is not finite as NaN.
+   whose moments are all below 2^-100 is held as 0, and one in which m or v is
+   not finite keeps neither: both are NaN from then on.
 
    SMORE_ADAMW_STOCHASTIC: codes and bf16 parameters are rounded up or down
    at random by their remainder (nearest, ties to even, without it), from a

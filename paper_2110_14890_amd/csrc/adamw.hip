@@ -16,7 +16,7 @@
 // where they are.  They are rounded stochastically instead, up with the
 // probability of the remainder, which is right in the mean.  A sqrt(v) that
 // is not 0 never gets the code 0, so that no later step divides by eps alone.
-// A value that is not finite makes the scale of its 128 elements NaN.
+// A moment that is not finite makes the scales of its 128 elements NaN.
 // Parameters in bf16 are rounded the same way.  The random bits are a hash
 // of (seed, step, tensor, block, element): nothing is kept between calls.
 #include <hip/hip_runtime.h>
@@ -177,8 +177,7 @@ __device__ __forceinline__ void decode(uint32_t four, float* out)
     out[3] = b[1];
 }
 
-// Largest magnitude of the 16 lanes of a block, as bits: NaN above infinity
-// above every number.
+// Largest of the 16 lanes of a block, as bits.
 __device__ __forceinline__ uint32_t block_max(uint32_t x)
 {
 #define SMORE_STEP(CTRL) x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true))
@@ -192,12 +191,11 @@ __device__ __forceinline__ uint32_t block_max(uint32_t x)
 
 // Scale of a block and the factor that takes its values to [0, 448].  Blocks
 // that have decayed below 2^-100 are 0, which keeps the factor finite.
-__device__ __forceinline__ void block_scale(uint32_t top_bits, float* scale, float* unit)
+__device__ __forceinline__ void block_scale(float top, bool lost, float* scale, float* unit)
 {
-    const float top = __uint_as_float(top_bits);
     const bool some = top >= 0x1p-100f;
     const float r = __builtin_amdgcn_rcpf(top);
-    *scale = top_bits >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : some ? top * (1.0f / 448.0f) : 0.0f;
+    *scale = lost ? __uint_as_float(0x7FC00000u) : some ? top * (1.0f / 448.0f) : 0.0f;
     // 1 / top to the nearest, as root_of()
     *unit = some ? fmaf(fmaf(-top, r, 1.0f), r, r) * 448.0f : 0.0f;
 }
@@ -326,12 +324,18 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
 #pragma unroll
         for (int j = 0; j < PER; ++j) draw[j] = mix(base + (uint32_t)j);
     }
-    // Adding to a NaN's lower bits could carry into its sign, and make it 0.
-    // A NaN of that kind comes with the gradient or the moments.
-    uint32_t m_top = 0;
+    uint32_t u_top = 0;   // largest root as bits: NaN above infinity above every number
 #pragma unroll
-    for (int j = 0; j < PER; ++j) m_top = max(m_top, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-    if (sizeof(TP) == 2 && stochastic && __any(m_top > 0x7F800000u)) {
+    for (int j = 0; j < PER; ++j) u_top = max(u_top, __float_as_uint(u[j]));
+    // Adding to a NaN's lower bits could carry into its sign, and make it 0.
+    // A NaN of that kind comes with the gradient, and makes the root one too,
+    // or with the first moment in 32 bits.
+    bool odd = u_top > 0x7F800000u;
+    if (BITS == 32) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) odd |= m[j] != m[j];
+    }
+    if (sizeof(TP) == 2 && stochastic && __any(odd)) {
 #pragma unroll
         for (int j = 0; j < PER; ++j)
             if (p[j] != p[j]) p[j] = __uint_as_float(0x7FC00000u);
@@ -344,12 +348,16 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
         }
     } else {
         // places behind the row's end were loaded as zeros and are 0 still
-        uint32_t u_top = 0;
+        float m_top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) u_top = max(u_top, __float_as_uint(u[j]) & 0x7FFFFFFFu);
+        for (int j = 0; j < PER; ++j) m_top = fmaxf(m_top, fabsf(m[j]));
+        u_top = block_max(u_top);
+        m_top = __uint_as_float(block_max(__float_as_uint(m_top)));
+        // a moment that is not finite, now or before, makes both NaN
+        const bool lost = u_top >= 0x7F800000u || !(m_top < INFINITY) || h.m_scale != h.m_scale;
         float m_scale, m_unit, u_scale, u_unit;
-        block_scale(block_max(m_top), &m_scale, &m_unit);
-        block_scale(block_max(u_top), &u_scale, &u_unit);
+        block_scale(m_top, lost, &m_scale, &m_unit);
+        block_scale(__uint_as_float(u_top), lost, &u_scale, &u_unit);
         float least = 448.0f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
