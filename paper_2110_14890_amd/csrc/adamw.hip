@@ -440,48 +440,52 @@ struct Entry {
     float w;
     uint32_t from;
 };
-__device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64_t end)
+__device__ __forceinline__ Entry entry_at(const RowsTensor& r, int64_t o, bool in)
 {
     Entry e{0.0f, 0u};
-    if (at < end) {
-        const int64_t o = r.order ? r.order[at] : at;
-        if (o >= 0 && o < r.n_entries) {   // a permutation's: reads nothing behind the gradients otherwise
-            e.w = r.coef ? r.coef[o] : 1.0f;
-            uint32_t q = (uint32_t)((double)o * r.per_inverse);   // off by one at most
-            if ((uint64_t)q * r.per > (uint64_t)o) --q;
-            if ((uint64_t)(q + 1) * r.per <= (uint64_t)o) ++q;
-            e.from = q;
-        }
+    if (in && o >= 0 && o < r.n_entries) {   // a permutation's: reads nothing behind the gradients otherwise
+        e.w = r.coef ? r.coef[o] : 1.0f;
+        uint32_t q = (uint32_t)((double)o * r.per_inverse);   // off by one at most
+        if ((uint64_t)q * r.per > (uint64_t)o) --q;
+        if ((uint64_t)(q + 1) * r.per <= (uint64_t)o) ++q;
+        e.from = q;
     }
     return e;
 }
+__device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64_t end)
+{
+    return entry_at(r, at < end && r.order ? r.order[at] : at, at < end);
+}
 
-// Adds the entries [first, end): products in fp32, their sum in 64 bits, so
-// that long runs lose nothing and the order does not show.
+// Adds the first n entries that the lanes hold: products in fp32, their sum
+// in 64 bits, so that long runs lose nothing and the order does not show.
+template <class TG>
+__device__ __forceinline__ void add_held(const RowsTensor& r, const Entry& e, int n, int64_t col, int have, double* g)
+{
+    for (int i = 0; i < n; i += AHEAD) {
+        float x[AHEAD][PER];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, min(i + q, n - 1));
+            load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            if (i + q >= n) break;
+            const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i + q));
+#pragma unroll
+            for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[q][j]);
+        }
+    }
+}
+// Adds the entries [first, end).
 template <class TG>
 __device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, int64_t end, int64_t col, int have,
                                             double* g)
 {
     const int lane = threadIdx.x & 63;
-    for (int64_t at = first; at < end; at += 64) {
-        const int n = (int)min((int64_t)64, end - at);
-        const Entry e = entry_of(r, at + lane, end);
-        for (int i = 0; i < n; i += AHEAD) {
-            float x[AHEAD][PER];
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, min(i + q, n - 1));
-                load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x[q]);
-            }
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                if (i + q >= n) break;
-                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i + q));
-#pragma unroll
-                for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[q][j]);
-            }
-        }
-    }
+    for (int64_t at = first; at < end; at += 64)
+        add_held<TG>(r, entry_of(r, at + lane, end), (int)min((int64_t)64, end - at), col, have, g);
 }
 
 // Sums of RUN consecutive entries of one row, where a run is that long, so
@@ -504,26 +508,15 @@ __global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, double* __r
     }
 }
 
-// A wavefront per entry, each a workgroup of its own; the first entry of a
-// row's run takes the row, the others end at once and leave their place.
-template <class TP, class TG, int BITS>
-__global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper)
-{
-    const int lane = threadIdx.x;
-    const int64_t i = blockIdx.x;
-    const int32_t row = r.rows[i];
-    if (row < 0 || row >= r.n_rows || (i > 0 && r.rows[i - 1] == row)) return;
-    Step s;
-    if (!step_of(hyper, r.t, &s)) return;
-    const bool stochastic = hyper.stochastic;
-    const bool single = i + 1 >= r.n_entries || r.rows[i + 1] != row;
-    const Entry only = entry_of(r, i, i + 1);
-    // [i, head): entries up to the run's end or the first sum made ahead;
-    // then `sums` of those; then [tail, end)
-    int64_t head = i + 1;
+// A run of one row's entries that is longer than a wavefront's first look.
+// [i, head): entries up to the run's end or the first sum made ahead; then
+// `sums` of those; then [tail, end).
+struct LongRun {
+    int64_t head, tail = 0, end = 0;
     int sums = 0;
-    int64_t tail = 0, end = 0;
-    if (!single) {
+    __device__ LongRun(const RowsTensor& r, int64_t i, int32_t row)
+    {
+        const int lane = threadIdx.x & 63;
         const int64_t next = (i + RUN - 1) / RUN * RUN;
         bool open = true;
         auto walk = [&](int64_t from, int64_t to) {   // the run's end within [from, to)
@@ -550,6 +543,33 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
             end = walk(tail, min(tail + RUN, r.n_entries));
         }
     }
+};
+
+// A wavefront per entry, each a workgroup of its own; the first entry of a
+// row's run takes the row, the others end at once and leave their place.
+// The first look is one read: the entry before, the run and its vectors'
+// numbers, up to LOOK entries on (most runs are shorter).
+constexpr int LOOK = 15;
+template <class TP, class TG, int BITS>
+__global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper)
+{
+    const int lane = threadIdx.x;
+    const int64_t i = blockIdx.x;
+    const int64_t look = i - 1 + lane, ahead = i + lane;
+    const bool in = lane < LOOK && ahead < r.n_entries;
+    int32_t id = -1;
+    if (lane <= LOOK && look >= 0 && look < r.n_entries) id = r.rows[look];
+    int64_t o = ahead;
+    if (in && r.order) o = r.order[ahead];
+    const int32_t row = __builtin_amdgcn_readlane(id, 1);
+    if (row < 0 || row >= r.n_rows || __builtin_amdgcn_readlane(id, 0) == row) return;
+    Step s;
+    if (!step_of(hyper, r.t, &s)) return;
+    const bool stochastic = hyper.stochastic;
+    const uint64_t same = __ballot(lane >= 1 && lane <= LOOK && id == row) >> 1;
+    const int length = __builtin_ctzll(~same);
+    const Entry e = entry_at(r, o, lane < length);
+
     const int64_t blocks = (r.dim + BLOCK - 1) / BLOCK;
     for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
         const int have = left(r.dim, col);
@@ -558,20 +578,27 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
         Held<BITS> h;
         load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
         load_held<BITS>(r.t, at, have, block, h);
-        if (single) {
-            load_floats<TG, PER>((const TG*)r.t.g + (int64_t)only.from * r.dim + col, have, g);
+        if (length == 1) {
+            const int64_t src = (uint32_t)__builtin_amdgcn_readfirstlane((int)e.from);
+            const float w = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(e.w)));
+            load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, g);
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] *= only.w;
+            for (int j = 0; j < PER; ++j) g[j] *= w;
         } else {
             double sum[PER] = {};
-            add_entries<TG>(r, i, head, col, have, sum);
-            const double* from = r.partial + (tail / RUN - sums) * r.dim + col;
-            for (int k = 0; k < sums; ++k, from += r.dim) {
+            if (length < LOOK) {
+                add_held<TG>(r, e, length, col, have, sum);
+            } else {
+                const LongRun run(r, i, row);
+                add_entries<TG>(r, i, run.head, col, have, sum);
+                const double* from = r.partial + (run.tail / RUN - run.sums) * r.dim + col;
+                for (int k = 0; k < run.sums; ++k, from += r.dim) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j)
-                    if (j < have) sum[j] += from[j];
+                    for (int j = 0; j < PER; ++j)
+                        if (j < have) sum[j] += from[j];
+                }
+                add_entries<TG>(r, run.tail, run.end, col, have, sum);
             }
-            add_entries<TG>(r, tail, end, col, have, sum);
 #pragma unroll
             for (int j = 0; j < PER; ++j) g[j] = (float)sum[j];
         }
