@@ -457,21 +457,22 @@ __device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64
     return entry_at(r, at < end && r.order ? r.order[at] : at, at < end);
 }
 
-// Adds the first n entries that the lanes hold: products in fp32, their sum
+// Adds the entries that lanes [first, end) hold: products in fp32, their sum
 // in 64 bits, so that long runs lose nothing and the order does not show.
 template <class TG>
-__device__ __forceinline__ void add_held(const RowsTensor& r, const Entry& e, int n, int64_t col, int have, double* g)
+__device__ __forceinline__ void add_held(const RowsTensor& r, const Entry& e, int first, int end, int64_t col, int have,
+                                         double* g)
 {
-    for (int i = 0; i < n; i += AHEAD) {
+    for (int i = first; i < end; i += AHEAD) {
         float x[AHEAD][PER];
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q) {
-            const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, min(i + q, n - 1));
+            const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, min(i + q, end - 1));
             load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x[q]);
         }
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q) {
-            if (i + q >= n) break;
+            if (i + q >= end) break;
             const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i + q));
 #pragma unroll
             for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[q][j]);
@@ -485,7 +486,7 @@ __device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, 
 {
     const int lane = threadIdx.x & 63;
     for (int64_t at = first; at < end; at += 64)
-        add_held<TG>(r, entry_of(r, at + lane, end), (int)min((int64_t)64, end - at), col, have, g);
+        add_held<TG>(r, entry_of(r, at + lane, end), 0, (int)min((int64_t)64, end - at), col, have, g);
 }
 
 // Sums of RUN consecutive entries of one row, where a run is that long, so
@@ -508,7 +509,7 @@ __global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, double* __r
     }
 }
 
-// A run of one row's entries that is longer than a wavefront's first look.
+// A run of one row's entries that goes on behind a wavefront's first look.
 // [i, head): entries up to the run's end or the first sum made ahead; then
 // `sums` of those; then [tail, end).
 struct LongRun {
@@ -545,64 +546,65 @@ struct LongRun {
     }
 };
 
-// A wavefront per entry, each a workgroup of its own; the first entry of a
-// row's run takes the row, the others end at once and leave their place.
-// The first look is one read: the entry before, the run and its vectors'
-// numbers, up to LOOK entries on (most runs are shorter).
-constexpr int LOOK = 15;
+// A wavefront per `window` entries (up to 16), each a workgroup of its own: it
+// steps the rows whose runs begin there.  Its first look is one read of the
+// entry before, the window, and what fits behind it, where most runs end.
 template <class TP, class TG, int BITS>
-__global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper)
+__global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper, int window)
 {
     const int lane = threadIdx.x;
-    const int64_t i = blockIdx.x;
-    const int64_t look = i - 1 + lane, ahead = i + lane;
-    const bool in = lane < LOOK && ahead < r.n_entries;
-    int32_t id = -1;
-    if (lane <= LOOK && look >= 0 && look < r.n_entries) id = r.rows[look];
-    int64_t o = ahead;
-    if (in && r.order) o = r.order[ahead];
-    const int32_t row = __builtin_amdgcn_readlane(id, 1);
-    if (row < 0 || row >= r.n_rows || __builtin_amdgcn_readlane(id, 0) == row) return;
+    const int64_t first = (int64_t)blockIdx.x * window;   // lane 1 looks at this entry
+    const int64_t look = first - 1 + lane;
+    const bool in = look >= 0 && look < r.n_entries;
+    const int32_t id = in ? r.rows[look] : -1;
+    const int64_t o = in && r.order ? r.order[look] : look;
+    const int32_t before = __shfl_up(id, 1);
+    const uint64_t begins = __ballot(lane > 0 && id != before);
+    uint64_t heads = __ballot(lane > 0 && lane <= window && id != before && id >= 0 && id < r.n_rows);
+    if (!heads) return;
     Step s;
     if (!step_of(hyper, r.t, &s)) return;
     const bool stochastic = hyper.stochastic;
-    const uint64_t same = __ballot(lane >= 1 && lane <= LOOK && id == row) >> 1;
-    const int length = __builtin_ctzll(~same);
-    const Entry e = entry_at(r, o, lane < length);
-
+    const Entry e = entry_at(r, o, in);
     const int64_t blocks = (r.dim + BLOCK - 1) / BLOCK;
-    for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
-        const int have = left(r.dim, col);
-        const int64_t at = (int64_t)row * r.dim + col, block = row * blocks + col / BLOCK;
-        float p[PER], g[PER];
-        Held<BITS> h;
-        load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
-        load_held<BITS>(r.t, at, have, block, h);
-        if (length == 1) {
-            const int64_t src = (uint32_t)__builtin_amdgcn_readfirstlane((int)e.from);
-            const float w = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(e.w)));
-            load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, g);
+    for (; heads; heads &= heads - 1) {
+        const int head = __builtin_ctzll(heads);
+        const int32_t row = __builtin_amdgcn_readlane(id, head);
+        const uint64_t later = head < 63 ? begins >> (head + 1) : 0;
+        const int end = later ? head + 1 + __builtin_ctzll(later) : 64;
+        for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
+            const int have = left(r.dim, col);
+            const int64_t at = (int64_t)row * r.dim + col, block = row * blocks + col / BLOCK;
+            float p[PER], g[PER];
+            Held<BITS> h;
+            load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
+            load_held<BITS>(r.t, at, have, block, h);
+            if (end == head + 1 && later) {
+                const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, head);
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), head));
+                load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, g);
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] *= w;
-        } else {
-            double sum[PER] = {};
-            if (length < LOOK) {
-                add_held<TG>(r, e, length, col, have, sum);
+                for (int j = 0; j < PER; ++j) g[j] *= w;
             } else {
-                const LongRun run(r, i, row);
-                add_entries<TG>(r, i, run.head, col, have, sum);
-                const double* from = r.partial + (run.tail / RUN - run.sums) * r.dim + col;
-                for (int k = 0; k < run.sums; ++k, from += r.dim) {
+                double sum[PER] = {};
+                if (later) {
+                    add_held<TG>(r, e, head, end, col, have, sum);
+                } else {
+                    const LongRun run(r, first - 1 + head, row);
+                    add_entries<TG>(r, first - 1 + head, run.head, col, have, sum);
+                    const double* from = r.partial + (run.tail / RUN - run.sums) * r.dim + col;
+                    for (int k = 0; k < run.sums; ++k, from += r.dim) {
 #pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        if (j < have) sum[j] += from[j];
+                        for (int j = 0; j < PER; ++j)
+                            if (j < have) sum[j] += from[j];
+                    }
+                    add_entries<TG>(r, run.tail, run.end, col, have, sum);
                 }
-                add_entries<TG>(r, run.tail, run.end, col, have, sum);
-            }
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] = (float)sum[j];
+                for (int j = 0; j < PER; ++j) g[j] = (float)sum[j];
+            }
+            step_held<TP, BITS>(r.t, s, stochastic, at, have, block, (int)(col % BLOCK), p, g, h);
         }
-        step_held<TP, BITS>(r.t, s, stochastic, at, have, block, (int)(col % BLOCK), p, g, h);
     }
 }
 
@@ -656,7 +658,14 @@ int rows_as(const smore_adamw_tensor& x, const Hyper& h, double* partial, hipStr
     r.per_inverse = 1.0 / r.per;
     const int64_t sums = x.n_entries / RUN;
     if (sums) k_run_sums<TG><<<(unsigned)((sums + WAVES - 1) / WAVES), WG, 0, st>>>(r, partial);
-    if (x.n_entries) k_adamw_rows<TP, TG, BITS><<<(unsigned)x.n_entries, 64, 0, st>>>(r, h);
+    // entries per wavefront: as many as leave each of the 1,024 SIMDs eight
+    // wavefronts.  8-bit moments, width 400, us with 1 / 4 / 16 entries:
+    // 1.05M entries of 371K rows 783 / 638 / 581, 264K of 156K 271 / 223 / 224;
+    // in 32 bits 66K of 14.4K 40 / 36 / 38.
+    int window = 1;
+    while (window < 16 && x.n_entries >= (int64_t)8192 * 2 * window) window *= 2;
+    if (x.n_entries)
+        k_adamw_rows<TP, TG, BITS><<<(unsigned)((x.n_entries + window - 1) / window), 64, 0, st>>>(r, h, window);
     return launched(err);
 }
 
