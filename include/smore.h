@@ -444,6 +444,17 @@ typedef struct {
 int smore_preference_loss(const smore_preference_args *args, const smore_preference_in *in,
                           const smore_preference_out *out, void *hip_stream);
 
+/* Stable order of n entries (0 .. 2^26 - 1) by the table row they name: rows
+   [n] receives ids (device int32 [n], any order) sorted, ids outside
+   [0, n_rows) last, and order [n] the entry each came from, equal ids in
+   their first order.  What smore_adamw takes as rows and order.  ids is not
+   written and must not overlap the outputs.  The workspace
+   (smore_sort_rows_workspace_bytes) is scratch after the call and not shared
+   by calls that overlap. */
+int smore_sort_rows_workspace_bytes(int64_t n, int32_t n_rows, size_t *bytes);
+int smore_sort_rows(const int32_t *ids, int64_t n, int32_t n_rows, int32_t *rows, int64_t *order,
+                    void *workspace, size_t ws_bytes, void *hip_stream);
+
 /* AdamW with decoupled weight decay, for many tensors in one call:
        m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
        p = p (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
@@ -451,8 +462,9 @@ int smore_preference_loss(const smore_preference_args *args, const smore_prefere
 
    A dense tensor (rows NULL) has n_rows x dim elements in a row, and so have
    its gradient and its moments.  A table (rows given) is stepped only in the
-   rows that a batch touched: rows (int32 [n_entries], ascending, repeats
-   allowed) names a row per entry, and the gradient of a row is the sum over
+   rows that a batch touched: rows (int32 [n_entries], ascending but for
+   entries outside [0, n_rows), which may come first or last; repeats allowed)
+   names a row per entry, and the gradient of a row is the sum over
    its entries i of coef[o] x grad[o / per], o = order[i], where grad is
    [ceil(n_entries / per), dim], order (int64) is a permutation of the
    entries (NULL: o = i) and coef is fp32 (NULL: 1).  With ids, grad_scores

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -148,13 +149,12 @@ def lib() -> ctypes.CDLL:
         L.smore_wait_before_kernel.argtypes = [c_vp, c_i32]
         L.smore_gather_probe.argtypes = [c_vp, c_i64, c_i64, c_vp, c_i64, c_vp]
         sp = ctypes.POINTER(ctypes.c_size_t)
-        L.smore_score.argtypes = [ctypes.POINTER(ScoreArgs)] + [c_vp] * 5
-        L.smore_score_grad_workspace_bytes.argtypes = [ctypes.POINTER(ScoreArgs), sp]
-        L.smore_score_grad.argtypes = [ctypes.POINTER(ScoreArgs)] + [c_vp] * 5 + [ctypes.c_size_t,
-                                                                                  c_vp]
-        L.smore_preference_loss.argtypes = [ctypes.POINTER(PreferenceArgs),
-                                            ctypes.POINTER(PreferenceIn),
-                                            ctypes.POINTER(PreferenceOut), c_vp]
+        L.smore_score.argtypes = [c_vp] * 6
+        L.smore_score_grad_workspace_bytes.argtypes = [c_vp, sp]
+        L.smore_score_grad.argtypes = [c_vp] * 6 + [ctypes.c_size_t, c_vp]
+        L.smore_preference_loss.argtypes = [c_vp] * 4
+        L.smore_sort_rows_workspace_bytes.argtypes = [c_i64, c_i32, sp]
+        L.smore_sort_rows.argtypes = [c_vp, c_i64, c_i32, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]
         L.smore_adamw_workspace_bytes.argtypes = [c_vp, c_i32, sp]
         L.smore_adamw.argtypes = [c_vp, c_i32, ctypes.POINTER(AdamWArgs), c_vp, ctypes.c_size_t,
                                   c_vp]
@@ -511,6 +511,19 @@ _torch = None
 _TYPES = {}          # element types of the C ABI
 
 
+def _packer(structure):
+    """struct.pack for a structure of the C ABI: the bytes of a call's
+    arguments in one step (filling a ctypes structure takes microseconds)."""
+    letters = {c_i32: "i", c_i64: "q", c_u32: "I", c_u64: "Q", c_vp: "P", ctypes.c_float: "f", ctypes.c_double: "d"}
+    packed = struct.Struct("@" + "".join(letters[kind] for _, kind in structure._fields_) + "0q")
+    assert packed.size == ctypes.sizeof(structure)
+    return packed.pack
+
+
+_pack_score, _pack_preference = _packer(ScoreArgs), _packer(PreferenceArgs)
+_pack_in, _pack_out = _packer(PreferenceIn), _packer(PreferenceOut)
+
+
 def _lazy_torch():
     global _torch
     if _torch is None:
@@ -566,8 +579,8 @@ def _ptr(t):
     return t.data_ptr() if t is not None and t.numel() else None
 
 
-def _score_args(table, candidates, other, other_name: str, grad_scores, grad_name: str) -> ScoreArgs:
-    """Checks and sizes of a score call: other [batch, dim], grad_scores [batch, n]."""
+def _score_args(table, candidates, other, other_name: str, grad_scores, grad_name: str) -> bytes:
+    """Checks and sizes (ScoreArgs) of a score call: other [batch, dim], grad_scores [batch, n]."""
     torch = _torch
     if table.dim() != 2 or candidates.dim() != 2:
         raise ValueError("table and candidates must be matrices")
@@ -585,9 +598,9 @@ def _score_args(table, candidates, other, other_name: str, grad_scores, grad_nam
         _operand(other_name, other, (batch, dim), wide, device)
         _operand(grad_name, grad_scores, shape, (torch.float32,), device)
     if batch > 1:     # rows of the candidates may coincide: one set for all queries
-        return ScoreArgs(batch, n, dim, v, _pitch(table, dim), other.stride(0), candidates.stride(0),
-                         grad_scores.stride(0), _TYPES[te], _TYPES[tq])
-    return ScoreArgs(batch, n, dim, v, _pitch(table, dim), dim, n, n, _TYPES[te], _TYPES[tq])
+        return _pack_score(batch, n, dim, v, _pitch(table, dim), other.stride(0), candidates.stride(0),
+                           grad_scores.stride(0), _TYPES[te], _TYPES[tq])
+    return _pack_score(batch, n, dim, v, _pitch(table, dim), dim, n, n, _TYPES[te], _TYPES[tq])
 
 
 def score_into(table, queries, candidates, scores, stream=None):
@@ -595,7 +608,7 @@ def score_into(table, queries, candidates, scores, stream=None):
     _lazy_torch()
     args = _score_args(table, candidates, queries, "queries", scores, "scores")
     _check(_launch(table.device, stream, lambda st: lib().smore_score(
-        ctypes.byref(args), _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st)))
+        args, _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st)))
     return scores
 
 
@@ -616,13 +629,13 @@ def score_grad_into(table, candidates, grad_scores, grad_queries, stream=None):
     torch = _lazy_torch()
     args = _score_args(table, candidates, grad_queries, "grad_queries", grad_scores, "grad_scores")
     L, need = lib(), ctypes.c_size_t()
-    _check(L.smore_score_grad_workspace_bytes(ctypes.byref(args), ctypes.byref(need)))
+    _check(L.smore_score_grad_workspace_bytes(args, ctypes.byref(need)))
     need = need.value
 
     def call(st):
         # a workspace of this call alone, from the stream's (or the capturing graph's) memory
         ws = torch.empty(need, dtype=torch.uint8, device=table.device) if need else None
-        return L.smore_score_grad(ctypes.byref(args), _ptr(table), _ptr(candidates), _ptr(grad_scores),
+        return L.smore_score_grad(args, _ptr(table), _ptr(candidates), _ptr(grad_scores),
                                   _ptr(grad_queries), _ptr(ws), need, st)
 
     _check(_launch(table.device, stream, call))
@@ -691,23 +704,15 @@ def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_
                           {"positive": positive, "negatives": negatives, "ref_positive": ref_positive,
                            "ref_negatives": ref_negatives, "grad_positive": grad_p, "grad_negatives": grad_n},
                           {"n_valid": n_valid, "mask": mask, "weight": weight, "loss": loss})
-    args = PreferenceArgs(batch, n, number, _TYPES[dtype], beta, smoothing, scale, positive.stride(0), negatives.stride(0))
-    ins = PreferenceIn(positive.data_ptr(), _ptr(negatives))
-    if ref_positive is not None:
-        args.ref_positive_stride, args.ref_negatives_stride = ref_positive.stride(0), ref_negatives.stride(0)
-        ins.ref_positive, ins.ref_negatives = ref_positive.data_ptr(), _ptr(ref_negatives)
-    if n_valid is not None:
-        ins.n_valid = n_valid.data_ptr()
-    if mask is not None:
-        ins.mask = _ptr(mask)
-    if weight is not None:
-        ins.weight = weight.data_ptr()
-    outs = PreferenceOut(loss.data_ptr() if loss is not None else None)
-    if grad_p is not None:
-        args.grad_positive_stride, args.grad_negatives_stride = grad_p.stride(0), grad_n.stride(0)
-        outs.grad_positive, outs.grad_negatives = grad_p.data_ptr(), _ptr(grad_n)
-    _check(_launch(device, stream, lambda st: lib().smore_preference_loss(
-        ctypes.byref(args), ctypes.byref(ins), ctypes.byref(outs), st)))
+    at = lambda t: 0 if t is None else t.data_ptr()
+    step = lambda t: 0 if t is None else t.stride(0)
+    if n == 0:
+        negatives = ref_negatives = grad_n = mask = None
+    args = _pack_preference(batch, n, number, _TYPES[dtype], beta, smoothing, scale, positive.stride(0), step(negatives),
+                            step(ref_positive), step(ref_negatives), step(grad_p), step(grad_n))
+    ins = _pack_in(positive.data_ptr(), at(negatives), at(ref_positive), at(ref_negatives), at(n_valid), at(mask), at(weight))
+    outs = _pack_out(at(loss), at(grad_p), at(grad_n))
+    _check(_launch(device, stream, lambda st: lib().smore_preference_loss(args, ins, outs, st)))
     return out
 
 
@@ -743,10 +748,11 @@ class RowGrad:
     """The gradient of a table in the rows that a batch touched: entry i of
     rows (int32, ascending, repeats allowed) adds coef[o] times
     grad[o // per], o = order[i], to its row (order int64 and coef fp32 by
-    entry, both optional).  Entries outside the table are skipped."""
+    entry, both optional).  Entries outside the table are skipped.  With
+    in_order False the rows may be in any order (order None): AdamW sorts them."""
 
-    def __init__(self, rows, grad, order=None, coef=None, per: int = 1):
-        self.rows, self.grad, self.order, self.coef, self.per = rows, grad, order, coef, per
+    def __init__(self, rows, grad, order=None, coef=None, per: int = 1, in_order: bool = True):
+        self.rows, self.grad, self.order, self.coef, self.per, self.in_order = rows, grad, order, coef, per, in_order
 
 
 def row_grad(ids, grad, coef=None, per: int = 1) -> RowGrad:
@@ -754,8 +760,26 @@ def row_grad(ids, grad, coef=None, per: int = 1) -> RowGrad:
     the flattened ids, adds coef[i] times grad[i // per].  With score()'s
     candidates [batch, n] as ids, its queries as grad, the gradient of its
     scores as coef and per = n this is score()'s gradient for the table."""
-    rows, order = _lazy_torch().sort(ids.reshape(-1), stable=True)
-    return RowGrad(rows, grad, order, None if coef is None else coef.reshape(-1), per)
+    return RowGrad(ids.reshape(-1), grad, None, None if coef is None else coef.reshape(-1), per, in_order=False)
+
+
+def sort_rows(ids, n_rows: int, stream=None):
+    """smore_sort_rows: (rows, order) of ids (int32 [n], contiguous) for a table
+    of n_rows rows: rows int32 ascending, ids outside the table last; order
+    int64, equal ids in their first order."""
+    torch = _lazy_torch()
+    if ids.dim() != 1 or ids.dtype != torch.int32 or not ids.is_contiguous():
+        raise ValueError(f"ids must be a contiguous int32 vector, got {ids.dtype} {tuple(ids.shape)}")
+    L, n, size = lib(), ids.numel(), ctypes.c_size_t()
+    _check(L.smore_sort_rows_workspace_bytes(n, n_rows, ctypes.byref(size)))
+
+    def call(st):
+        new = lambda count, dtype: torch.empty(count, dtype=dtype, device=ids.device)
+        rows, order, ws = new(n, torch.int32), new(n, torch.int64), new(size.value, torch.uint8)
+        _check(L.smore_sort_rows(_ptr(ids), n, n_rows, _ptr(rows), _ptr(order), _ptr(ws), size.value, st))
+        return rows, order
+
+    return _launch(ids.device, stream, call)
 
 
 def alloc_adamw_state(param, bits: int = 32, table: bool = False) -> dict:
@@ -865,7 +889,7 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        used, device, scaled, tables = [], self.device, self.bits == 8, False
+        used, device, scaled, tables, sorts = [], self.device, self.bits == 8, False, []
         for k, g in enumerate(grads):
             if g is None:
                 continue
@@ -877,7 +901,8 @@ class AdamW:
                                                                         or state["v_scale"].data_ptr() != seen[6])):
                 self._describe(k)
             if type(g) is RowGrad:
-                self._rows(k, self._items[k], p, g)
+                if not self._rows(k, self._items[k], p, g, stream, sorts):
+                    continue
                 tables = True
             else:
                 if g.shape != shape or g.dtype not in _TYPES or g.device != device or not g.is_contiguous():
@@ -926,7 +951,10 @@ class AdamW:
         # autograd sees that they changed
         torch.autograd.graph.increment_version([p for p in (self.params[k] for k in used) if not p.is_inference()])
 
-    def _rows(self, k: int, x, p, g: RowGrad) -> None:
+    def _rows(self, k: int, x, p, g: RowGrad, stream, kept: list) -> bool:
+        """Puts a RowGrad into the list, and what the call has to keep into
+        kept; False if it has no entries (whose address may be NULL, which
+        would stand for a dense gradient)."""
         torch = _torch
         if p.dim() != 2 or not self._by_rows[k]:
             raise ValueError(f"parameter {k} is no table with moments per row: its gradient cannot be a RowGrad")
@@ -942,6 +970,13 @@ class AdamW:
                 g.grad.dtype not in _TYPES or g.grad.device != self.device or not g.grad.is_contiguous():
             raise ValueError(f"gradient {k} must hold contiguous rows of {p.shape[1]} on {self.device}, one for each "
                              f"{g.per} of {n} entries, got {g.grad.dtype} {tuple(g.grad.shape)} on {g.grad.device}")
-        x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), _TYPES[g.grad.dtype], g.rows.data_ptr(), \
-            None if g.order is None else g.order.data_ptr(), None if g.coef is None else g.coef.data_ptr()
+        if not g.in_order and g.order is not None:
+            raise ValueError(f"gradient {k} has an order, but its rows are not in order")
+        if n == 0:
+            return False
+        rows, order = (g.rows, g.order) if g.in_order else sort_rows(g.rows, p.shape[0], stream)
+        kept.append((rows, order))
+        x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), _TYPES[g.grad.dtype], rows.data_ptr(), \
+            None if order is None else order.data_ptr(), None if g.coef is None else g.coef.data_ptr()
         x.n_entries, x.per, self._last[k] = n, g.per, RowGrad
+        return True

@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsmore.so")
 SOURCES = ["capi.cpp", "graph_build.hip", "sample.hip", "probe.hip", "score.hip", "loss.hip",
-           "adamw.hip"]
+           "sort_rows.hip", "adamw.hip"]
 ARCH = os.environ.get("SMORE_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [

@@ -2,7 +2,7 @@
 // validation, the fourteen plan presets, the node-cut planner, compilation of a
 // plan into the positive-sampling program, and graph handle management; and
 // the checks of the training calls.  Device work is in graph_build.hip and
-// sample.hip, and in score.hip, loss.hip and adamw.hip.
+// sample.hip, and in score.hip, loss.hip, sort_rows.hip and adamw.hip.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -828,6 +828,29 @@ int smore_preference_loss(const smore_preference_args* a, const smore_preference
     const char* err = "";
     rc = smore::launch_preference(*a, *in, *out, (hipStream_t)hip_stream, &err);
     return rc ? fail(rc, "smore_preference_loss: %s", err) : ok();
+}
+
+int smore_sort_rows_workspace_bytes(int64_t n, int32_t n_rows, size_t* bytes)
+{
+    if (!bytes) return fail(SMORE_E_INVALID_ARG, "bytes is NULL");
+    if (n < 0 || n_rows < 1) return fail(SMORE_E_INVALID_ARG, "need n >= 0 and n_rows >= 1");
+    if (n >= (int64_t)1 << 26) return fail(SMORE_E_OVERFLOW, "entries must stay below 2^26");
+    *bytes = smore::sort_rows_workspace(n, n_rows);
+    return ok();
+}
+
+int smore_sort_rows(const int32_t* ids, int64_t n, int32_t n_rows, int32_t* rows, int64_t* order, void* workspace,
+                    size_t ws_bytes, void* hip_stream)
+{
+    size_t need = 0;
+    const int rc = smore_sort_rows_workspace_bytes(n, n_rows, &need);
+    if (rc) return rc;
+    if (n == 0) return ok();
+    if (!ids || !rows || !order) return fail(SMORE_E_INVALID_ARG, "a buffer is NULL");
+    if (!workspace || ws_bytes < need) return fail(SMORE_E_INVALID_ARG, "workspace missing or smaller than %zu bytes", need);
+    const char* err = "";
+    const int launch = smore::launch_sort_rows(ids, n, n_rows, rows, order, workspace, (hipStream_t)hip_stream, &err);
+    return launch ? fail(launch, "smore_sort_rows: %s", err) : ok();
 }
 
 int smore_adamw_workspace_bytes(const smore_adamw_tensor* ts, int32_t n, size_t* bytes)

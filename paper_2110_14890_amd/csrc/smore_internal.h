@@ -145,7 +145,7 @@ int scratch_workspace(void** ptr, size_t* bytes, const char** err);
 int64_t gather_probe_threads(int64_t n_reads);
 int launch_gather_probe(const void* table, int64_t table_bytes, int64_t n_reads, uint32_t* sink,
                         hipStream_t st, const char** err);
-// score.hip, loss.hip, adamw.hip: arguments as checked by capi.cpp
+// score.hip, loss.hip, sort_rows.hip, adamw.hip: arguments as checked by capi.cpp
 int launch_score(const smore_score_args& a, const void* table, const void* queries,
                  const int32_t* ids, float* scores, hipStream_t st, const char** err);
 size_t score_grad_workspace(const smore_score_args& a);
@@ -153,6 +153,9 @@ int launch_score_grad(const smore_score_args& a, const void* table, const int32_
                       const float* grad, void* out, void* ws, hipStream_t st, const char** err);
 int launch_preference(const smore_preference_args& p, const smore_preference_in& in,
                       const smore_preference_out& out, hipStream_t st, const char** err);
+size_t sort_rows_workspace(int64_t n, int32_t n_rows);
+int launch_sort_rows(const int32_t* ids, int64_t n, int32_t n_rows, int32_t* rows, int64_t* order,
+                     void* ws, hipStream_t st, const char** err);
 size_t adamw_workspace(const smore_adamw_tensor* ts, int n);
 int launch_adamw(const smore_adamw_tensor* ts, int n, const smore_adamw_args& a, void* ws,
                  hipStream_t st, const char** err);

@@ -137,6 +137,20 @@ def test_adamw_overlap_and_workspace(L):
     assert adamw(L, []) == 0                                      # nothing to do
 
 
+def test_sort_rows(L):
+    n = ctypes.c_size_t()
+    for count, rows, code in ((-1, 5, -1), (3, 0, -1), (2 ** 26, 5, -6)):
+        assert L.smore_sort_rows_workspace_bytes(count, rows, ctypes.byref(n)) == code
+        assert L.smore_sort_rows(P, count, rows, P, P, P, 1 << 30, None) == code
+    assert L.smore_sort_rows_workspace_bytes(1000, 5, ctypes.byref(n)) == 0 and n.value >= 16 * 1000
+    assert L.smore_sort_rows(P, 1000, 5, P, P, P, n.value - 1, None) == -1 and "workspace" in sm.last_error()
+    for k in range(3):
+        p = [P, P, P]
+        p[k] = None
+        assert L.smore_sort_rows(p[0], 1000, 5, p[1], p[2], P, n.value, None) == -1 and "NULL" in sm.last_error()
+    assert L.smore_sort_rows(None, 0, 5, None, None, None, 0, None) == 0                       # nothing to do
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     import torch
     table, q = torch.zeros(5, 4), torch.zeros(2, 4)
