@@ -457,55 +457,99 @@ __device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64
     return entry_at(r, at < end && r.order ? r.order[at] : at, at < end);
 }
 
-// Adds the entries that lanes [first, end) hold: products in fp32, their sum
-// in 64 bits, so that long runs lose nothing and the order does not show.
-template <class TG>
-__device__ __forceinline__ void add_held(const RowsTensor& r, const Entry& e, int first, int end, int64_t col, int have,
-                                         double* g)
-{
-    for (int i = first; i < end; i += AHEAD) {
-        float x[AHEAD][PER];
+// Sums over a row's entries: products in fp32, their sum in 64 bits, so that
+// long runs lose nothing and the order does not show.  Rows of at most MOST
+// lanes (below 64) take as few lanes as hold them, a power of two; 64 / lanes
+// groups add every so many entries each, and finish() adds the groups' sums.
+template <class TG, int MOST>
+struct RowSum {
+    const RowsTensor& r;
+    int64_t col;
+    int lanes, group, groups, have;
+    double g[PER];
+
+    __device__ __forceinline__ RowSum(const RowsTensor& t, int64_t chunk) : r(t)
+    {
+        const int lane = threadIdx.x & 63;
+        lanes = MOST;
+        if (MOST < 64)
+            while (lanes > 1 && (lanes / 2) * PER >= r.dim) lanes /= 2;
+        group = MOST < 64 ? lane / lanes : 0;
+        groups = 64 / lanes;
+        col = chunk + (lane % lanes) * PER;
+        have = left(r.dim, col);
 #pragma unroll
-        for (int q = 0; q < AHEAD; ++q) {
-            const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, min(i + q, end - 1));
-            load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x[q]);
-        }
+        for (int j = 0; j < PER; ++j) g[j] = 0.0;
+    }
+
+    // x of lane `at`, the same one for all lanes of a group
+    __device__ __forceinline__ int from_lane(int x, int at) const
+    {
+        return MOST == 64 ? __builtin_amdgcn_readlane(x, at) : __shfl(x, at);
+    }
+    // the entries that lanes [first, end) hold
+    __device__ __forceinline__ void held(const Entry& e, int first, int end)
+    {
+        for (int i = first + group; i - group < end; i += AHEAD * groups) {
+            float x[AHEAD][PER];
 #pragma unroll
-        for (int q = 0; q < AHEAD; ++q) {
-            if (i + q >= end) break;
-            const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), i + q));
+            for (int q = 0; q < AHEAD; ++q) {
+                const int64_t src = (uint32_t)from_lane((int)e.from, min(i + q * groups, end - 1));
+                load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, x[q]);
+            }
 #pragma unroll
-            for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[q][j]);
+            for (int q = 0; q < AHEAD; ++q) {
+                const float w = __int_as_float(from_lane(__float_as_int(e.w), min(i + q * groups, end - 1)));
+                if (i + q * groups < end) {
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) g[j] += (double)(w * x[q][j]);
+                }
+            }
         }
     }
-}
-// Adds the entries [first, end).
-template <class TG>
-__device__ __forceinline__ void add_entries(const RowsTensor& r, int64_t first, int64_t end, int64_t col, int have,
-                                            double* g)
-{
-    const int lane = threadIdx.x & 63;
-    for (int64_t at = first; at < end; at += 64)
-        add_held<TG>(r, entry_of(r, at + lane, end), 0, (int)min((int64_t)64, end - at), col, have, g);
-}
+    // the entries [first, end) of the list
+    __device__ __forceinline__ void entries(int64_t first, int64_t end)
+    {
+        const int lane = threadIdx.x & 63;
+        for (int64_t at = first; at < end; at += 64) held(entry_of(r, at + lane, end), 0, (int)min((int64_t)64, end - at));
+    }
+    // the sums made ahead of `count` stretches of RUN entries
+    __device__ __forceinline__ void ahead(int64_t first, int count)
+    {
+        for (int k = group; k < count; k += groups) {
+            const double* from = r.partial + (first + k) * r.dim + col;
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (j < have) g[j] += from[j];
+        }
+    }
+    __device__ __forceinline__ void finish()
+    {
+        for (int d = lanes; d < 64; d *= 2) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) g[j] += __shfl_xor(g[j], d);
+        }
+    }
+};
 
 // Sums of RUN consecutive entries of one row, where a run is that long, so
 // that no wavefront has to add a hub's entries one by one.
-template <class TG>
+template <class TG, int MOST>
 __global__ __launch_bounds__(WG) void k_run_sums(const RowsTensor r, double* __restrict__ partial)
 {
-    const int lane = threadIdx.x & 63;
     const int64_t c = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
     if ((c + 1) * RUN > r.n_entries) return;
     const int32_t row = r.rows[c * RUN];
     if (row < 0 || row >= r.n_rows || r.rows[c * RUN + RUN - 1] != row) return;
-    for (int64_t col = lane * PER; col - lane * PER < r.dim; col += CHUNK) {
-        const int have = left(r.dim, col);
-        double g[PER] = {};
-        add_entries<TG>(r, c * RUN, (c + 1) * RUN, col, have, g);
+    for (int64_t chunk = 0; chunk < r.dim; chunk += CHUNK) {
+        RowSum<TG, MOST> sum(r, chunk);
+        sum.entries(c * RUN, (c + 1) * RUN);
+        sum.finish();
+        if (sum.group == 0) {
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (j < have) partial[c * r.dim + col + j] = g[j];
+            for (int j = 0; j < PER; ++j)
+                if (j < sum.have) partial[c * r.dim + sum.col + j] = sum.g[j];
+        }
     }
 }
 
@@ -549,7 +593,10 @@ struct LongRun {
 // A wavefront per `window` entries (up to 16), each a workgroup of its own: it
 // steps the rows whose runs begin there.  Its first look is one read of the
 // entry before, the window, and what fits behind it, where most runs end.
-template <class TP, class TG, int BITS>
+// Rows that LANES lanes hold (16 or 32: up to 128 or 256 columns) are stepped
+// 64 / LANES at a time, where their runs are short; the others one by one.
+constexpr int SHORT = 4;
+template <class TP, class TG, int BITS, int LANES>
 __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper, int window)
 {
     const int lane = threadIdx.x;
@@ -567,6 +614,51 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
     const bool stochastic = hyper.stochastic;
     const Entry e = entry_at(r, o, in);
     const int64_t blocks = (r.dim + BLOCK - 1) / BLOCK;
+    if constexpr (LANES < 64) {
+        const uint64_t after = lane < 63 ? begins >> (lane + 1) : 0;
+        const int mine = after ? __builtin_ctzll(after) + 1 : 64;      // entries of the run that begins here
+        uint64_t quick = heads & __ballot(mine <= SHORT);
+        heads &= ~quick;
+        while (quick) {
+            const int group = lane / LANES, col = lane % LANES * PER;
+            int head = -1;
+#pragma unroll
+            for (int q = 0; q < 64 / LANES; ++q) {
+                if (quick && group == q) head = __builtin_ctzll(quick);
+                quick &= quick - 1;
+            }
+            // every lane takes part in the exchanges, those without a row too
+            const int32_t named = __shfl(id, head & 63), length = __shfl(mine, head & 63);
+            const int64_t row = head < 0 ? 0 : named;
+            const int count = head < 0 ? 0 : length;
+            const int have = head < 0 ? 0 : left(r.dim, col);
+            const int64_t at = row * r.dim + col, block = row * blocks + col / BLOCK;
+            float p[PER], g[PER];
+            Held<BITS> h;
+            {
+                double sum[PER] = {};
+                float x[SHORT][PER], w[SHORT];
+#pragma unroll
+                for (int k = 0; k < SHORT; ++k) {
+                    const int from = (head + k) & 63;
+                    const int64_t src = (uint32_t)__shfl((int)e.from, from);
+                    w[k] = __shfl(e.w, from);
+                    load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, k < count ? have : 0, x[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < SHORT; ++k)
+                    if (k < count) {
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) sum[j] += (double)(w[k] * x[k][j]);
+                    }
+#pragma unroll
+                for (int j = 0; j < PER; ++j) g[j] = (float)sum[j];
+            }
+            load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
+            load_held<BITS>(r.t, at, have, block, h);
+            step_held<TP, BITS>(r.t, s, stochastic, at, have, block, col % BLOCK, p, g, h);
+        }
+    }
     for (; heads; heads &= heads - 1) {
         const int head = __builtin_ctzll(heads);
         const int32_t row = __builtin_amdgcn_readlane(id, head);
@@ -577,6 +669,20 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
             const int64_t at = (int64_t)row * r.dim + col, block = row * blocks + col / BLOCK;
             float p[PER], g[PER];
             Held<BITS> h;
+            if (!(end == head + 1 && later)) {
+                RowSum<TG, LANES> sum(r, col - lane * PER);
+                if (later) {
+                    sum.held(e, head, end);
+                } else {
+                    const LongRun run(r, first - 1 + head, row);
+                    sum.entries(first - 1 + head, run.head);
+                    sum.ahead(run.tail / RUN - run.sums, run.sums);
+                    sum.entries(run.tail, run.end);
+                }
+                sum.finish();
+#pragma unroll
+                for (int j = 0; j < PER; ++j) g[j] = (float)sum.g[j];
+            }
             load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
             load_held<BITS>(r.t, at, have, block, h);
             if (end == head + 1 && later) {
@@ -585,23 +691,6 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
                 load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, g);
 #pragma unroll
                 for (int j = 0; j < PER; ++j) g[j] *= w;
-            } else {
-                double sum[PER] = {};
-                if (later) {
-                    add_held<TG>(r, e, head, end, col, have, sum);
-                } else {
-                    const LongRun run(r, first - 1 + head, row);
-                    add_entries<TG>(r, first - 1 + head, run.head, col, have, sum);
-                    const double* from = r.partial + (run.tail / RUN - run.sums) * r.dim + col;
-                    for (int k = 0; k < run.sums; ++k, from += r.dim) {
-#pragma unroll
-                        for (int j = 0; j < PER; ++j)
-                            if (j < have) sum[j] += from[j];
-                    }
-                    add_entries<TG>(r, run.tail, run.end, col, have, sum);
-                }
-#pragma unroll
-                for (int j = 0; j < PER; ++j) g[j] = (float)sum[j];
             }
             step_held<TP, BITS>(r.t, s, stochastic, at, have, block, (int)(col % BLOCK), p, g, h);
         }
@@ -657,15 +746,21 @@ int rows_as(const smore_adamw_tensor& x, const Hyper& h, double* partial, hipStr
     r.per = (uint32_t)(x.per < (1 << 30) ? x.per : 1 << 30);   // entries are fewer
     r.per_inverse = 1.0 / r.per;
     const int64_t sums = x.n_entries / RUN;
-    if (sums) k_run_sums<TG><<<(unsigned)((sums + WAVES - 1) / WAVES), WG, 0, st>>>(r, partial);
+    const unsigned sum_grid = (unsigned)((sums + WAVES - 1) / WAVES);
+    if (sums && x.dim <= 32 * PER) k_run_sums<TG, 32><<<sum_grid, WG, 0, st>>>(r, partial);
+    else if (sums) k_run_sums<TG, 64><<<sum_grid, WG, 0, st>>>(r, partial);
     // entries per wavefront: as many as leave each of the 1,024 SIMDs eight
     // wavefronts.  8-bit moments, width 400, us with 1 / 4 / 16 entries:
     // 1.05M entries of 371K rows 783 / 638 / 581, 264K of 156K 271 / 223 / 224;
     // in 32 bits 66K of 14.4K 40 / 36 / 38.
     int window = 1;
     while (window < 16 && x.n_entries >= (int64_t)8192 * 2 * window) window *= 2;
-    if (x.n_entries)
-        k_adamw_rows<TP, TG, BITS><<<(unsigned)((x.n_entries + window - 1) / window), 64, 0, st>>>(r, h, window);
+    const unsigned grid = (unsigned)((x.n_entries + window - 1) / window);
+    if (x.n_entries) {
+        if (x.dim <= 16 * PER) k_adamw_rows<TP, TG, BITS, 16><<<grid, 64, 0, st>>>(r, h, window);
+        else if (x.dim <= 32 * PER) k_adamw_rows<TP, TG, BITS, 32><<<grid, 64, 0, st>>>(r, h, window);
+        else k_adamw_rows<TP, TG, BITS, 64><<<grid, 64, 0, st>>>(r, h, window);
+    }
     return launched(err);
 }
 
