@@ -434,8 +434,9 @@ typedef struct {
    the gradient of row b's loss: grad_positive [B], grad_negatives [B, n]
    (both NULL: not wanted).  A row without a valid negative has loss and
    gradients 0; places that are not valid are not used and get gradient 0.
-   A valid score that is NaN makes its row NaN, as in the formula.  Outputs
-   must not overlap inputs or each other. */
+   A valid score that is NaN makes its row NaN, as in the formula, and so does
+   a negative at +infinity with SMORE_PREFERENCE_SOFTMAX.  Outputs must not
+   overlap inputs or each other. */
 typedef struct {
     float *loss;
     void *grad_positive, *grad_negatives;
@@ -518,10 +519,12 @@ typedef struct {
 
 /* Steps n_tensors (host array) tensors.  Parameters and moments must not
    overlap, neither within a tensor nor between tensors: of the parameters
-   this is checked (SMORE_E_INVALID_ARG).  The workspace holds sums of long
-   runs of equal rows (0 bytes without tables; scratch after the call, not
-   shared by calls that overlap).  SMORE_E_OVERFLOW: 2^26 or more entries, or
-   2^34 or more elements. */
+   this is checked (SMORE_E_INVALID_ARG).  That rows ascends is not: of a row
+   that is named again after another one, some entries would be lost.  The
+   workspace holds sums of long runs of equal rows (0 bytes without tables;
+   scratch after the call, not shared by calls that overlap).
+   SMORE_E_OVERFLOW: 2^26 or more entries, table rows of more than 2^20
+   columns, or 2^34 or more elements of a dense tensor. */
 int smore_adamw_workspace_bytes(const smore_adamw_tensor *tensors, int32_t n_tensors, size_t *bytes);
 int smore_adamw(const smore_adamw_tensor *tensors, int32_t n_tensors, const smore_adamw_args *args,
                 void *workspace, size_t ws_bytes, void *hip_stream);

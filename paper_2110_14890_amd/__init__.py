@@ -505,6 +505,10 @@ def gather_probe(table, n_reads: int, stream=None):
 
 
 # ------------------------------------------------- training on sampled batches
+# Gradients are outputs and inputs of these calls, as the C ABI has them:
+# autograd does not see the calls (torch.autograd.backward(queries,
+# score_grad(...)) goes on into a model's own graph).
+#
 # Small calls take as long as this binding does, so the checks of a call are
 # plain comparisons; what is wrong is spelled out only where one fails.
 _torch = None
@@ -976,6 +980,10 @@ class AdamW:
             return False
         rows, order = (g.rows, g.order) if g.in_order else sort_rows(g.rows, p.shape[0], stream)
         kept.append((rows, order))
+        if stream is not None:      # what row_grad made may be freed before that stream gets here
+            for t in (g.rows, g.grad, g.order, g.coef):
+                if t is not None:
+                    t.record_stream(stream)
         x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), _TYPES[g.grad.dtype], rows.data_ptr(), \
             None if order is None else order.data_ptr(), None if g.coef is None else g.coef.data_ptr()
         x.n_entries, x.per, self._last[k] = n, g.per, RowGrad

@@ -749,6 +749,7 @@ int check_adamw_tensor(const smore_adamw_tensor& t, int k)
         return SMORE_OK;
     }
     if (t.n_rows > INT32_MAX) return fail(SMORE_E_OVERFLOW, "tensor %d: n_rows must be an int32", k);
+    if (t.dim > (1 << 20)) return fail(SMORE_E_OVERFLOW, "tensor %d: rows of a table have at most 2^20 columns", k);
     if (t.n_entries < 0) return fail(SMORE_E_INVALID_ARG, "tensor %d: n_entries must be >= 0", k);
     if (t.n_entries >= (int64_t)1 << 26) return fail(SMORE_E_OVERFLOW, "tensor %d: entries must stay below 2^26", k);
     if (t.n_entries > 0 && !t.grad) return fail(SMORE_E_INVALID_ARG, "tensor %d: grad is NULL", k);

@@ -203,6 +203,31 @@ def check_sums(p1, s1, p0, s0, g, dg, param, bits, step, row):
         assert (np.abs(decode(s1[name], s1[name + "_scale"]) - x) <= (code_step * 2.001 * scale[at]) + dx).all(), (row, name)
 
 
+@pytest.mark.parametrize("dim", [3, 24, 200, 300])
+def test_a_hub_among_the_entries(dim):
+    """One row with 20,000 entries (sums made ahead of more stretches than a
+    wavefront looks at at once), from an odd place, among short runs."""
+    import torch
+    rng = np.random.default_rng(dim)
+    dev = torch.device("cuda")
+    rows = 200
+    ids = np.concatenate([np.full(20_000, 77), rng.integers(0, rows, size=3001)]).astype(np.int32)
+    rng.shuffle(ids)
+    n = len(ids)
+    p = torch.as_tensor(rng.normal(size=(rows, dim)) * 0.05, dtype=torch.float32, device=dev)
+    state = start_state(rng, p, 32, True)
+    opt = sm.AdamW([p], **OPT, states=[state], steps=10)
+    vectors = torch.as_tensor(rng.normal(size=(-(-n // 7), dim)), dtype=torch.float32, device=dev)
+    coef = f32(rng.uniform(0.5, 1.0, size=n) * 1e-5)
+    before = snapshot(p, state)
+    opt.step([sm.row_grad(torch.as_tensor(ids, device=dev), vectors, coef=torch.as_tensor(coef, device=dev), per=7)])
+    p1, s1 = snapshot(p, state)
+    sums, off = sum_entries(ids, coef.astype(float), as64(vectors), 7, rows)
+    for r in range(rows):
+        row = lambda d: {k: a[r] for k, a in d.items()}
+        check_sums(p1[r], row(s1), before[0][r], row(before[1]), sums[r], off[r], "float32", 32, 11, r)
+
+
 def test_rows_equal_a_dense_step():
     """Every row of a table of whole blocks named once, in a shuffled order:
     the same bits as a dense step of it."""

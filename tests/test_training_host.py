@@ -110,7 +110,8 @@ def adamw(L, tensors, **kw):
     (dict(param_type=3), -3), (dict(grad_type=3), -3), (dict(bits=16), -3), (dict(bits=8), -1), (dict(n_rows=0), -1),
     (dict(dim=0), -1), (dict(weight_decay=NAN), -1), (dict(n_rows=2 ** 33, dim=2), -6), (dict(n_rows=2 ** 62, dim=2 ** 62), -6),
     (dict(rows=P, n_entries=-1), -1), (dict(rows=P, n_entries=2 ** 26), -6), (dict(rows=P, n_entries=4, per=0), -1),
-    (dict(rows=P, n_entries=4, grad=None), -1), (dict(rows=P, n_rows=2 ** 31), -6)])
+    (dict(rows=P, n_entries=4, grad=None), -1), (dict(rows=P, n_rows=2 ** 31), -6),
+    (dict(rows=P, n_entries=4, dim=2 ** 20 + 1), -6)])
 def test_adamw_tensors(L, fields, code):
     n = ctypes.c_size_t()
     bad = tensor(**fields)
