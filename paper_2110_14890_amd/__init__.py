@@ -797,6 +797,8 @@ def alloc_adamw_state(param, bits: int = 32, table: bool = False) -> dict:
         return {k: new(tuple(param.shape), torch.float32) for k in ("m", "v")}
     if bits != 8:
         raise ValueError(f"moments have 8 or 32 bits, not {bits}")
+    if table and param.dim() != 2:
+        raise ValueError(f"a table has rows and columns, not shape {tuple(param.shape)}")
     blocks = lambda n: -(-n // ADAMW_BLOCK)
     shape = (param.shape[0], blocks(param.shape[1])) if table else (blocks(param.numel()),)
     state = {k: new(tuple(param.shape), torch.uint8).view(torch.float8_e4m3fn) for k in ("m", "v")}

@@ -401,7 +401,10 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
 __device__ __forceinline__ int left(int64_t end, int64_t at) { return (int)max((int64_t)0, min((int64_t)PER, end - at)); }
 
 // A workgroup takes WAVES x CHUNKS chunks of one tensor; which one it finds
-// among the launch's tensors by their first workgroups.
+// among the launch's tensors by their first workgroups.  320M elements, bf16
+// parameters and gradients, 8-bit moments: 590 us, 5.5 TB/s, with vector
+// operations in 88 % of the issue slots (54 an element, a third of them the
+// hash of the roundings); 15 tensors of 1.1M elements in 32 bits: 10 us.
 template <class TP, class TG, int BITS, int CHUNKS>
 __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper hyper)
 {
@@ -595,6 +598,9 @@ struct LongRun {
 // entry before, the window, and what fits behind it, where most runs end.
 // Rows that LANES lanes hold (16 or 32: up to 128 or 256 columns) are stepped
 // 64 / LANES at a time, where their runs are short; the others one by one.
+// 156K rows of 400 (264K entries), 8-bit moments: 230 us; 14.4K rows (66K
+// entries) in 32 bits: 37 us, 3.7 TB/s.  The first is bound by the vector
+// operations of k_adamw in 50 of 64 lanes, the second by the MALL.
 constexpr int SHORT = 4;
 template <class TP, class TG, int BITS, int LANES>
 __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper, int window)

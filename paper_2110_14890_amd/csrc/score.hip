@@ -142,6 +142,10 @@ struct Sums {
 // time, U times over before the first is used, are multiplied with the query,
 // which stays in registers, and summed over the LANES lanes.  Lane k keeps
 // packed candidate k's score, so that the scores leave in one store.
+// 8,192 x 257 candidates (a quarter of them padding) of a 2 GB table of rows
+// of 400 bf16: 239 us, 6.1 TB/s of 128-byte lines, of 6.5 to 7.1 that reads at
+// random places reach; 425 with four wavefronts per workgroup, whose places a
+// query short of negatives kept, and padding not packed away.
 template <class TE, class TQ, int LANES, int V, int NI, int U>
 __global__ __launch_bounds__(64) void k_score(const TE* __restrict__ table, int64_t table_stride, int rows, int dim,
                                               const TQ* __restrict__ queries, int64_t query_stride,
@@ -200,6 +204,8 @@ __global__ __launch_bounds__(64) void k_score(const TE* __restrict__ table, int6
 // its columns; its wavefronts deal the candidates out 64 at a time and add
 // their sums in LDS.  Several workgroups that share a query (splits > 1:
 // few queries with long lists) write partial sums, which k_join adds.
+// 4,096 x 257 candidates of 400,000 rows of 400 fp32: 197 us, 6.9 TB/s of
+// lines, the MALL's among them; 16 x 4,001 of width 200 in bf16: 8 + 3 us.
 template <class TE, class TO, int LANES, int V, int NI, int U>
 __global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table, int64_t table_stride, int rows, int dim,
                                                    const int32_t* __restrict__ ids, int64_t id_stride,

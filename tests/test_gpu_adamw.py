@@ -387,6 +387,53 @@ def test_capture_with_counts_on_the_device():
         assert (t_a - t_b).abs().max().item() <= (k + 1) * (1e-3 * 16 * 32 * EPS32 + 8 * EPS32 * 5)
 
 
+def test_rate_on_the_device_and_decay_per_parameter():
+    """A rate in an fp32 tensor equals the same number given as one (which has
+    to be an fp32 number): the step size's quotient is a product then, one
+    rounding more."""
+    import torch
+    rng = np.random.default_rng(26)
+    dev = torch.device("cuda")
+    rate = 2.0 ** -9
+    start = torch.as_tensor(rng.normal(size=900), dtype=torch.float32, device=dev)
+    g = torch.as_tensor(rng.normal(size=900), dtype=torch.float32, device=dev)
+    ps = [start.clone() for _ in range(4)]
+    sm.AdamW(ps[:2], lr=rate, weight_decay=[0.0, 0.5]).step([g, g])
+    lr = torch.tensor([rate], device=dev)
+    opt = sm.AdamW(ps[2:], lr=lr, weight_decay=[0.0, 0.5])
+    opt.step([g, g])
+    for x, y in ((ps[0], ps[2]), (ps[1], ps[3])):
+        assert ((x - y).abs() <= rate * 2 * EPS32 + 2 * EPS32 * x.abs()).all()
+    # decay takes rate x 0.5 of the parameter: within three roundings of it
+    assert ((ps[0] - ps[1] - start * (rate * 0.5)).abs() <= 4 * EPS32 * start.abs() + rate * 2 * EPS32).all()
+    lr.fill_(0.0)
+    before = ps[2].clone()
+    opt.step([g, g])
+    assert torch.equal(before, ps[2])
+
+
+def test_a_parameter_that_was_replaced():
+    """Addresses are not kept: a parameter's data and a state's tensors may be
+    replaced between steps."""
+    import torch
+    dev = torch.device("cuda")
+    p = torch.ones(300, device=dev)
+    opt = sm.AdamW([p], **OPT)
+    g = torch.full((300,), 0.5, device=dev)
+    opt.step([g])
+    old = p.data
+    p.data = torch.full((300,), 2.0, device=dev)
+    opt.states[0]["m"] = torch.zeros(300, device=dev)
+    kept = old.clone()
+    opt.step([g])
+    assert torch.equal(old, kept) and (p < 2.0).all() and opt.states[0]["m"].any()
+    p.data = torch.zeros(10, device=dev)
+    with pytest.raises(ValueError, match="fits"):
+        opt.step([torch.zeros(10, device=dev)])
+    with pytest.raises(ValueError, match="table"):
+        sm.AdamW([torch.zeros(10, device=dev)], bits=8, tables=(0,))
+
+
 def test_a_table_beyond_32_bit_offsets():
     """Rows whose elements lie behind the 2^32nd, with a run across the
     length whose sums are made ahead."""

@@ -158,3 +158,45 @@ def test_gradient_is_the_slope_of_the_scores():
         rise = (sm.score(td, unit, idd).double() * w.double()).sum(1)      # exact products of one column
         size = (sm.score(td.abs(), unit, idd).double() * w.double().abs()).sum(1)
         assert ((grad[:, c].double() - rise).abs() <= 8 * EPS32 * size).all()
+
+
+def test_capture_and_replay():
+    """A captured call whose queries are split over workgroups (its workspace
+    lies in the graph's memory), replayed on new inputs with other calls of
+    that kind between."""
+    import torch
+    rng = np.random.default_rng(7)
+    dev = torch.device("cuda")
+    t, q, ids = make(rng, 300, 72, 3, 2000, "float32", "float32")
+    td, idd = t.to(dev), torch.as_tensor(ids, device=dev)
+    g = torch.zeros((3, 2000), device=dev)
+    sm.score_grad(td, idd, g)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = sm.score_grad(td, idd, g)
+    for _ in range(4):
+        g.copy_(torch.as_tensor(rng.normal(size=(3, 2000))))
+        idd.copy_(torch.as_tensor(rng.integers(-1, 301, size=(3, 2000))))
+        graph.replay()
+        other = sm.score_grad(td, idd.flip(1).contiguous(), g)
+        torch.cuda.synchronize()
+        assert torch.equal(out, sm.score_grad(td, idd, g)) and not torch.equal(out, other)
+
+
+def test_calls_side_by_side_on_streams():
+    """Split calls that overlap do not share scratch memory."""
+    import torch
+    rng = np.random.default_rng(8)
+    dev = torch.device("cuda")
+    t, _, _ = make(rng, 3000, 400, 1, 1, "bfloat16", "float32")
+    td = t.to(dev)
+    ids = [torch.as_tensor(rng.integers(-1, 3000, size=(4, 4000)), dtype=torch.int32, device=dev) for _ in range(4)]
+    g = [torch.as_tensor(rng.normal(size=(4, 4000)), dtype=torch.float32, device=dev) for _ in range(4)]
+    want = [sm.score_grad(td, i, x) for i, x in zip(ids, g)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    for _ in range(5):
+        got = [sm.score_grad(td, i, x, stream=s) for i, x, s in zip(ids, g, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

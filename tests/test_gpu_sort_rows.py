@@ -69,3 +69,27 @@ def test_empty_and_in_a_step():
     two.steps = one.steps - 1            # the step without entries counted
     two.step([sm.row_grad(ids, vec, per=7)])
     assert torch.equal(a, b)
+
+
+def test_a_captured_step_sorts_its_entries():
+    """Unsorted entries in a captured step: each replay sorts what the ids hold
+    then; eager steps between use the same sizes."""
+    import torch
+    rng = np.random.default_rng(4)
+    dev = torch.device("cuda")
+    ids = torch.zeros((90, 11), dtype=torch.int32, device=dev)
+    vec = torch.as_tensor(rng.normal(size=(90, 70)), dtype=torch.float32, device=dev)
+    a, b = torch.ones((60, 70), device=dev), torch.ones((60, 70), device=dev)
+    kw = dict(tables=(0,), device_step=True, bits=8, seed=1)
+    graphed, eager = sm.AdamW([a], **kw), sm.AdamW([b], **kw)
+    sm.AdamW([torch.ones((60, 70), device=dev)], **kw).step([sm.row_grad(ids, vec, per=11)])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step([sm.row_grad(ids, vec, per=11)])
+    for k in range(4):
+        ids.copy_(torch.as_tensor(rng.integers(-1, 61, size=(90, 11))))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager.step([sm.row_grad(ids, vec, per=11)])
+        assert torch.equal(a, b), k
