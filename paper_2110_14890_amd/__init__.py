@@ -678,6 +678,13 @@ def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_
     """smore_preference_loss into the caller's tensors: out has "loss" (fp32
     [batch]), or "grad_positive" [batch] and "grad_negatives" [batch, n] of
     the scores' type, or all three."""
+    return _preference(positive, negatives, out, ref_positive, ref_negatives, n_valid, mask, kind, beta, smoothing,
+                       weight, stream, False)
+
+
+def _preference(positive, negatives, out, ref_positive, ref_negatives, n_valid, mask, kind, beta, smoothing, weight,
+                stream, fits: bool) -> dict:
+    """The call behind preference_loss; fits: out is known to."""
     torch = _lazy_torch()
     number = PREFERENCE_KINDS.get(kind)
     if number is None:
@@ -701,8 +708,8 @@ def preference_loss_into(positive, negatives, out: dict, ref_positive=None, ref_
         and (n_valid is None or (_fits(n_valid, row, i32, at) and n_valid.is_contiguous())) \
         and (mask is None or (_fits(mask, (batch, (n + 31) // 32), i32, at) and mask.is_contiguous())) \
         and (weight is None or (_fits(weight, row, f32, at) and weight.is_contiguous())) \
-        and (loss is None or (_fits(loss, row, f32, at) and loss.is_contiguous())) \
-        and (grad_p is None or (_fits(grad_p, row, dtype, at) and _fits(grad_n, shape, dtype, at)))
+        and (fits or ((loss is None or (_fits(loss, row, f32, at) and loss.is_contiguous()))
+                      and (grad_p is None or (_fits(grad_p, row, dtype, at) and _fits(grad_n, shape, dtype, at)))))
     if not good:
         _check_preference(batch, n, dtype, device,
                           {"positive": positive, "negatives": negatives, "ref_positive": ref_positive,
@@ -736,16 +743,16 @@ def preference_loss(positive, negatives, ref_positive=None, ref_negatives=None, 
     torch = _lazy_torch()
 
     def new(_):
-        rows, device = negatives.shape[:1], negatives.device
-        out = {"loss": torch.empty(rows, dtype=torch.float32, device=device)}
+        shape = negatives.shape
+        out = {"loss": negatives.new_empty(shape[:1], dtype=torch.float32)}
         if grad:
-            out["grad_positive"] = torch.empty(rows, dtype=negatives.dtype, device=device)
-            out["grad_negatives"] = torch.empty(negatives.shape, dtype=negatives.dtype, device=device)
+            out["grad_positive"] = negatives.new_empty(shape[:1])
+            out["grad_negatives"] = negatives.new_empty(shape)
         return out
 
     out = new(None) if stream is None else _launch(negatives.device, stream, new)
-    return preference_loss_into(positive, negatives, out, ref_positive, ref_negatives, n_valid, mask, kind, beta,
-                                smoothing, weight, stream)
+    return _preference(positive, negatives, out, ref_positive, ref_negatives, n_valid, mask, kind, beta, smoothing,
+                       weight, stream, True)
 
 
 class RowGrad:

@@ -41,14 +41,14 @@ constexpr int AHEAD = 4;                // vectors of a run in flight
 // One step's constants.
 struct Step {
     float rate, keep, b1, b2, a1, a2, eps;   // a = 1 - b
-    float move, root;                        // rate / (1 - b1^t), 1 / sqrt(1 - b2^t)
+    float slope, floor;                      // of the step's divisor, see divisor()
     float scale;                             // of the gradients
     uint32_t key;
 };
 
 struct Hyper {
-    Step s;                             // as the host knows it (keep and move for decay 0)
-    float log_b1, log_b2;
+    Step s;                             // as the host knows it (keep for decay 0)
+    float c1, c2, log_b1, log_b2;       // c = 1 - b^t
     const int64_t* step;                // step, rate and gradient scale on the device, or NULL
     const float* lr_dev;
     const float* grad_scale;
@@ -100,20 +100,32 @@ __host__ __device__ inline uint32_t step_key(uint32_t seed_key, int64_t t)
 }
 
 // The step's constants for one tensor; false where nothing is to be written.
+// A step's size, rate (m / c1) / (sqrt(v / c2) + eps), as m / -(slope sqrt(v) +
+// floor): one product fewer.  A rate whose reciprocal is not finite stands
+// still.
+__host__ __device__ inline void divisor(Step* s, float c1, float c2)
+{
+    s->slope = -c1 / (s->rate * sqrtf(c2));
+    s->floor = -c1 * s->eps / s->rate;
+    if (!(fabsf(s->slope) < INFINITY) || !(fabsf(s->floor) < INFINITY)) {
+        s->slope = 0.0f;
+        s->floor = -INFINITY;
+    }
+}
+
 __device__ __forceinline__ bool step_of(const Hyper& h, const Tensor& t, Step* s)
 {
     *s = h.s;
     if (h.on_device) {
-        if (h.lr_dev) {
-            s->move *= *h.lr_dev;       // the host's is of rate 1
-            s->rate = *h.lr_dev;
-        }
+        if (h.lr_dev) s->rate = *h.lr_dev;
+        float c1 = h.c1, c2 = h.c2;
         if (h.step) {
             const int64_t at = *h.step;
-            s->move = s->rate / -expm1f((float)at * h.log_b1);
-            s->root = 1.0f / sqrtf(-expm1f((float)at * h.log_b2));
+            c1 = -expm1f((float)at * h.log_b1);
+            c2 = -expm1f((float)at * h.log_b2);
             s->key = step_key(h.seed_key, at);
         }
+        divisor(s, c1, c2);
         if (h.grad_scale) s->scale = *h.grad_scale;
         if (!(fabsf(s->scale) < INFINITY)) return false;
     }
@@ -315,7 +327,7 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
         m[j] = first_moment(m[j], g[j], s);
         v[j] = second_moment(v[j], g[j], s);
         u[j] = BITS == 8 ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
-        p[j] = fmaf(-s.move * m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.root, s.eps)), p[j] * s.keep);
+        p[j] = fmaf(m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.slope, s.floor)), p[j] * s.keep);
     }
     constexpr bool DRAWS = BITS == 8 || sizeof(TP) == 2;
     uint32_t draw[PER] = {};
@@ -806,8 +818,9 @@ int launch_adamw(const smore_adamw_tensor* ts, int n, const smore_adamw_args& a,
     h.s.a1 = (float)(1.0 - a.beta1);
     h.s.a2 = (float)(1.0 - a.beta2);
     h.s.eps = (float)a.eps;
-    h.s.move = (float)((a.lr_device ? 1.0 : a.lr) / -expm1((double)a.step * log(a.beta1)));
-    h.s.root = (float)(1.0 / sqrt(-expm1((double)a.step * log(a.beta2))));
+    h.c1 = (float)-expm1((double)a.step * log(a.beta1));
+    h.c2 = (float)-expm1((double)a.step * log(a.beta2));
+    divisor(&h.s, h.c1, h.c2);
     h.s.scale = 1.0f;
     h.log_b1 = (float)log(a.beta1);
     h.log_b2 = (float)log(a.beta2);
