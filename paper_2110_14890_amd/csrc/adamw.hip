@@ -609,8 +609,9 @@ struct LongRun {
 // steps the rows whose runs begin there.  Its first look is one read of the
 // entry before, the window, and what fits behind it, where most runs end.
 // Rows that LANES lanes hold (16 or 32: up to 128 or 256 columns) are stepped
-// 64 / LANES at a time, where their runs are short; the others one by one.
-// 156K rows of 400 (264K entries), 8-bit moments: 230 us; 14.4K rows (66K
+// 64 / LANES at a time, where their runs are short; wider ones that one chunk
+// holds two at a time; the others one by one.
+// 156K rows of 400 (264K entries), 8-bit moments: 194 us; 14.4K rows (66K
 // entries) in 32 bits: 37 us, 3.7 TB/s.  The first is bound by the vector
 // operations of k_adamw in 50 of 64 lanes, the second by the MALL.
 constexpr int SHORT = 4;
@@ -675,6 +676,52 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
             load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
             load_held<BITS>(r.t, at, have, block, h);
             step_held<TP, BITS>(r.t, s, stochastic, at, have, block, col % BLOCK, p, g, h);
+        }
+    }
+    if (LANES == 64 && r.dim <= CHUNK) {
+        // rows with few entries two at a time, so that the second's reads are
+        // on their way while the first is stepped: 194 us instead of 230 for the
+        // 156K rows, 9.1 ms instead of 9.9 for 7.9M rows of 86M, and 562 instead
+        // of 557 where most runs have three entries (one-by-one below that: pairs
+        // of single entries alone 203 and 601)
+        const uint64_t after = lane < 63 ? begins >> (lane + 1) : 0;
+        const int mine = after ? __builtin_ctzll(after) + 1 : 64;      // entries of the run that begins here
+        uint64_t quick = heads & __ballot(mine <= SHORT);
+        const int col = lane * PER, have = left(r.dim, col);
+        while (quick & (quick - 1)) {
+            float p[2][PER], g[2][PER];
+            Held<BITS> h[2];
+            int64_t at[2], block[2];
+            int head[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                head[q] = __builtin_ctzll(quick);
+                heads &= ~(quick & (0 - quick));
+                quick &= quick - 1;
+                const int64_t row = __builtin_amdgcn_readlane(id, head[q]);
+                at[q] = row * r.dim + col;
+                block[q] = row * blocks + col / BLOCK;
+                load_floats<TP, PER>((const TP*)r.t.p + at[q], have, p[q]);
+                load_held<BITS>(r.t, at[q], have, block[q], h[q]);
+                const int64_t src = (uint32_t)__builtin_amdgcn_readlane((int)e.from, head[q]);
+                load_floats<TG, PER>((const TG*)r.t.g + src * r.dim + col, have, g[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.w), head[q]));
+#pragma unroll
+                for (int j = 0; j < PER; ++j) g[q][j] *= w;
+                const int count = __builtin_amdgcn_readlane(mine, head[q]);
+                if (count > 1) {
+                    RowSum<TG, LANES> sum(r, 0);
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) sum.g[j] = g[q][j];
+                    sum.held(e, head[q] + 1, head[q] + count);
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) g[q][j] = (float)sum.g[j];
+                }
+                step_held<TP, BITS>(r.t, s, stochastic, at[q], have, block[q], col % BLOCK, p[q], g[q], h[q]);
+            }
         }
     }
     for (; heads; heads &= heads - 1) {
@@ -768,9 +815,10 @@ int rows_as(const smore_adamw_tensor& x, const Hyper& h, double* partial, hipStr
     if (sums && x.dim <= 32 * PER) k_run_sums<TG, 32><<<sum_grid, WG, 0, st>>>(r, partial);
     else if (sums) k_run_sums<TG, 64><<<sum_grid, WG, 0, st>>>(r, partial);
     // entries per wavefront: as many as leave each of the 1,024 SIMDs eight
-    // wavefronts.  8-bit moments, width 400, us with 1 / 4 / 16 entries:
-    // 1.05M entries of 371K rows 783 / 638 / 581, 264K of 156K 271 / 223 / 224;
-    // in 32 bits 66K of 14.4K 40 / 36 / 38.
+    // wavefronts, up to 16.  8-bit moments, width 400, us with 1 / 4 / 8 / 16 /
+    // 32 entries: 1.05M entries of 371K rows 844 / 693 / 653 / 634 / 613, 263K
+    // of 250K 439 / 305 / 296 / 296 / 316; in 32 bits 66K of 14.9K
+    // 48 / 41 / 41 / 45 / 47.
     int window = 1;
     while (window < 16 && x.n_entries >= (int64_t)8192 * 2 * window) window *= 2;
     const unsigned grid = (unsigned)((x.n_entries + window - 1) / window);
