@@ -358,7 +358,7 @@ int smore_gather_probe(const void *table, int64_t table_bytes, int64_t n_reads, 
 enum { SMORE_F32 = 0, SMORE_BF16 = 1, SMORE_F16 = 2 };
 
 /* Sizes of smore_score / smore_score_grad.
-   batch B (>= 1), n candidates per query (>= 0), dim (1 .. 2^20);
+   batch B (>= 1), n candidates per query (0 .. 2^30), dim (1 .. 2^20);
    n_rows        rows V of the table (>= 1)
    table_stride, query_stride (>= dim), candidate_stride, score_stride
                  (>= n): distance of two rows; the rows of the candidates

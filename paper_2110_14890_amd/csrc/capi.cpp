@@ -685,7 +685,7 @@ int check_score(const smore_score_args* a)
 {
     if (!a) return fail(SMORE_E_INVALID_ARG, "args is NULL");
     if (a->batch < 1) return fail(SMORE_E_INVALID_ARG, "batch must be >= 1");
-    if (a->n < 0) return fail(SMORE_E_INVALID_ARG, "n must be >= 0");
+    if (a->n < 0 || a->n > (1 << 30)) return fail(SMORE_E_INVALID_ARG, "n must be in [0, 2^30]");
     if (a->dim < 1 || a->dim > (1 << 20)) return fail(SMORE_E_INVALID_ARG, "dim must be in [1, 2^20]");
     if (a->n_rows < 1) return fail(SMORE_E_INVALID_ARG, "n_rows must be >= 1");
     if (a->table_stride < a->dim || a->query_stride < a->dim || a->candidate_stride < 0 ||

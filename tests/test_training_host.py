@@ -58,6 +58,24 @@ def test_score_pointers_and_limits(L):
     assert L.smore_score_grad_workspace_bytes(ctypes.byref(score_args(batch=4096)), ctypes.byref(n)) == 0 and n.value == 0
 
 
+@pytest.mark.parametrize("n", [2 ** 30 + 1, 2 ** 31 - 8, 2 ** 31 - 7, 2 ** 31 - 1])
+@pytest.mark.parametrize("batch", [1, 600])
+def test_score_lists_that_are_too_long(L, n, batch):
+    """Lengths whose sums with a tile's or a share's size pass 31 bits."""
+    a = ctypes.byref(score_args(batch=batch, n=n, candidate_stride=0, score_stride=n))
+    size = ctypes.c_size_t()
+    assert L.smore_score(a, P, P, P, P, None) == -1 and "2^30" in sm.last_error()
+    assert L.smore_score_grad_workspace_bytes(a, ctypes.byref(size)) == -1 and "2^30" in sm.last_error()
+    assert L.smore_score_grad(a, P, P, P, P, P, 2 ** 62, None) == -1 and "2^30" in sm.last_error()
+
+
+def test_the_longest_score_lists(L):
+    a = ctypes.byref(score_args(batch=1, n=2 ** 30, candidate_stride=0, score_stride=2 ** 30))
+    size = ctypes.c_size_t()
+    assert L.smore_score(a, P, P, P, P, None) == -6
+    assert L.smore_score_grad_workspace_bytes(a, ctypes.byref(size)) == 0 and size.value == 512 * 8 * 4
+
+
 def preference(L, args=(), ins=(), outs=()):
     a = dict(batch=4, n=3, kind=0, score_type=0, beta=0.5, smoothing=0.0, scale=1.0, positive_stride=1, negatives_stride=3,
              ref_positive_stride=1, ref_negatives_stride=3, grad_positive_stride=1, grad_negatives_stride=3)
