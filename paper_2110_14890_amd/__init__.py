@@ -825,7 +825,8 @@ class AdamW:
     the step count is kept in an int64 device tensor, counted up by a kernel,
     so that a captured step counts when it is replayed.
 
-    Moments are in .states, the count in .steps (.device_steps)."""
+    Moments are in .states, the count in .steps (.device_steps); .lr, .betas,
+    .eps and .weight_decay may be changed between steps."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  bits: int = 32, seed: "int | None" = None, tables=(), states=None, steps: int = 0,
@@ -833,10 +834,7 @@ class AdamW:
         torch = _lazy_torch()
         self.params = list(params)
         self.lr, self.betas, self.eps, self.seed, self.steps = lr, betas, eps, seed, steps
-        self.weight_decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else \
-            [weight_decay] * len(self.params)
-        if len(self.weight_decay) != len(self.params):
-            raise ValueError("weight_decay is a number or one per parameter")
+        self.weight_decay, self._decays = self._decay_list(weight_decay), None
         if not self.params:
             raise ValueError("no parameters")
         self.device = self.params[0].device
@@ -853,8 +851,22 @@ class AdamW:
         self._list = (AdamWTensor * n)()
         self._items = [self._list[k] for k in range(n)]
         self._seen, self._by_rows, self._whole, self._last, self._empty = ([None] * n for _ in range(5))
+        self._take_decays()
         for k in range(n):
             self._describe(k)
+
+    def _decay_list(self, decay) -> list:
+        decays = list(decay) if isinstance(decay, (list, tuple)) else [decay] * len(self.params)
+        if len(decays) != len(self.params):
+            raise ValueError("weight_decay is a number or one per parameter")
+        return decays
+
+    def _take_decays(self) -> None:
+        """Puts the parameters' decays into the list."""
+        self.weight_decay = self._decay_list(self.weight_decay)
+        self._decays = list(self.weight_decay)
+        for x, decay in zip(self._items, self._decays):
+            x.weight_decay = decay
 
     def _describe(self, k: int) -> None:
         """Checks parameter k and its moments and puts them into the list."""
@@ -888,7 +900,7 @@ class AdamW:
         x.param, x.m, x.v = p.data_ptr(), state["m"].data_ptr(), state["v"].data_ptr()
         x.m_scale, x.v_scale = (state["m_scale"].data_ptr(), state["v_scale"].data_ptr()) if self.bits == 8 else (None, None)
         x.n_rows, x.dim = (p.shape[0], p.shape[1]) if p.dim() == 2 else (1, p.numel())
-        x.param_type, x.bits, x.index, x.weight_decay = _TYPES[p.dtype], self.bits, k, self.weight_decay[k]
+        x.param_type, x.bits, x.index = _TYPES[p.dtype], self.bits, k
         self._seen[k] = [p.shape, p] + [t.data_ptr() for t in (p, *(state[n] for n in shapes))]
         self._by_rows[k], self._whole[k], self._last[k], self._empty[k] = by_rows, whole, None, p.numel() == 0
 
@@ -903,15 +915,17 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
         used, device, scaled, tables, sorts = [], self.device, self.bits == 8, False, []
+        if self.weight_decay != self._decays:
+            self._take_decays()
         for k, g in enumerate(grads):
             if g is None:
                 continue
             p, state, seen = self.params[k], self.states[k], self._seen[k]
             shape = p.shape
             # a parameter or moments that were replaced are looked at again
-            if p is not seen[1] or shape != seen[0] or p.data_ptr() != seen[2] or state["m"].data_ptr() != seen[3] \
-                    or state["v"].data_ptr() != seen[4] or (scaled and (state["m_scale"].data_ptr() != seen[5]
-                                                                        or state["v_scale"].data_ptr() != seen[6])):
+            if p is not seen[1] or shape != seen[0] or not p.is_contiguous() or p.data_ptr() != seen[2] \
+                    or state["m"].data_ptr() != seen[3] or state["v"].data_ptr() != seen[4] or \
+                    (scaled and (state["m_scale"].data_ptr() != seen[5] or state["v_scale"].data_ptr() != seen[6])):
                 self._describe(k)
             if type(g) is RowGrad:
                 if not self._rows(k, self._items[k], p, g, stream, sorts):

@@ -434,6 +434,41 @@ def test_a_parameter_that_was_replaced():
         sm.AdamW([torch.zeros(10, device=dev)], bits=8, tables=(0,))
 
 
+def test_settings_that_change_between_steps():
+    """Rate, decay, betas and eps are those of the object at the step."""
+    import torch
+    dev = torch.device("cuda")
+    p = [torch.ones(40, device=dev), torch.ones(40, device=dev)]
+    opt = sm.AdamW(p, lr=0.5, weight_decay=[0.0, 0.0])
+    zero = [torch.zeros(40, device=dev)] * 2
+    opt.step(zero)
+    assert all((x == 1.0).all() for x in p)
+    opt.weight_decay[1] = 0.5
+    opt.step(zero)
+    assert (p[0] == 1.0).all() and (p[1] == 0.75).all()
+    opt.lr, opt.weight_decay = 0.25, [1.0, 0.0]
+    opt.step(zero)
+    assert (p[0] == 0.75).all() and (p[1] == 0.75).all()
+    opt.lr, opt.weight_decay = 1.0, 0.5
+    opt.step(zero)
+    assert all((x == 0.375).all() for x in p) and opt.weight_decay == [0.5, 0.5]
+    opt.weight_decay = [1.0]
+    with pytest.raises(ValueError, match="weight_decay"):
+        opt.step(zero)
+    assert all((x == 0.375).all() for x in p) and opt.steps == 4
+
+
+def test_a_parameter_that_is_no_longer_contiguous():
+    import torch
+    dev = torch.device("cuda")
+    p = torch.ones(6, 6, device=dev)
+    opt = sm.AdamW([p], **OPT)
+    opt.step([torch.ones(6, 6, device=dev)])
+    p.data = p.data.t()
+    with pytest.raises(ValueError, match="contiguous"):
+        opt.step([torch.ones(6, 6, device=dev)])
+
+
 def test_a_table_beyond_32_bit_offsets():
     """Rows whose elements lie behind the 2^32nd, with a run across the
     length whose sums are made ahead."""
