@@ -743,6 +743,12 @@ def preference_loss(positive, negatives, ref_positive=None, ref_negatives=None, 
     torch = _lazy_torch()
 
     def new(_):
+        if positive.is_contiguous() and negatives.is_contiguous():      # 9.0 us a call instead of 10.7
+            like = torch.empty_like
+            if grad:
+                return {"loss": like(positive, dtype=torch.float32), "grad_positive": like(positive),
+                        "grad_negatives": like(negatives)}
+            return {"loss": like(positive, dtype=torch.float32)}
         shape = negatives.shape
         out = {"loss": negatives.new_empty(shape[:1], dtype=torch.float32)}
         if grad:
