@@ -359,7 +359,8 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
             store_floats<float, PER>((float*)t.v + at, have, v);
         }
     } else {
-        // places behind the row's end were loaded as zeros and are 0 still
+        // places behind the row's end were loaded as zeros, have no gradient
+        // and are 0 still
         float m_top = 0.0f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) m_top = fmaxf(m_top, fabsf(m[j]));
@@ -745,8 +746,11 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
                     sum.entries(run.tail, run.end);
                 }
                 sum.finish();
+                // Rows of at most 64 columns are summed by groups of fewer than 16
+                // lanes: what a lane without a column has of it is another lane's,
+                // and must not count in their block's largest moment.
 #pragma unroll
-                for (int j = 0; j < PER; ++j) g[j] = (float)sum.g[j];
+                for (int j = 0; j < PER; ++j) g[j] = have > 0 ? (float)sum.g[j] : 0.0f;
             }
             load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
             load_held<BITS>(r.t, at, have, block, h);
