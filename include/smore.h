@@ -503,6 +503,9 @@ typedef struct {
 } smore_adamw_tensor;
 
 /* lr (finite, >= 0), beta1, beta2 in [0, 1), eps (finite, >= 0), step t (>= 1).
+   With eps 0 the quotient of an element whose v is 0 is infinite or NaN: one
+   without any gradient yet, or of gradients whose squares vanish in fp32 (below
+   about 1e-21 in a first step with beta2 0.999).
    On the device, for steps captured into a graph (NULL: not used):
    step_device (int64, >= 1) and lr_device (fp32) replace step and lr;
    grad_scale (fp32) multiplies every gradient, and where it is not finite

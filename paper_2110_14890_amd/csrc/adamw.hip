@@ -144,6 +144,16 @@ __device__ __forceinline__ float root_of(float v)
     const float s = v * r;
     return fmaf(fmaf(-s, s, v), 0.5f * r, s);
 }
+// A root of the moments' width.  The hardware's roots take a subnormal number
+// for 0, or here for the least normal one: v of a gradient below 3e-18 in the
+// first step.  Such a v is scaled first; with an eps of that size or 0 the
+// parameter would go to infinity otherwise.
+template <int BITS>
+__device__ __forceinline__ float root(float v)
+{
+    return BITS == 8 ? root_of(v) : __builtin_amdgcn_sqrtf(v);
+}
+constexpr int SUBNORMAL = 0x80;   // of v_cmp_class, positive ones
 
 __device__ __forceinline__ float first_moment(float m, float g, const Step& s)
 {
@@ -299,6 +309,7 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
                                           int64_t block, int j0, float* p, float* g, Held<BITS>& h)
 {
     float m[PER], v[PER], u[PER];
+    bool rare = false;   // a v whose root takes more than the hardware's
     if (s.scale != 1.0f) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) g[j] *= s.scale;
@@ -326,9 +337,16 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
     for (int j = 0; j < PER; ++j) {
         m[j] = first_moment(m[j], g[j], s);
         v[j] = second_moment(v[j], g[j], s);
-        u[j] = BITS == 8 ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
-        p[j] = fmaf(m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.slope, s.floor)), p[j] * s.keep);
+        u[j] = root<BITS>(v[j]);
+        rare |= __builtin_amdgcn_classf(v[j], SUBNORMAL);
     }
+    if (__any(rare)) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (__builtin_amdgcn_classf(v[j], SUBNORMAL)) u[j] = root<BITS>(v[j] * 0x1p64f) * 0x1p-32f;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) p[j] = fmaf(m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.slope, s.floor)), p[j] * s.keep);
     constexpr bool DRAWS = BITS == 8 || sizeof(TP) == 2;
     uint32_t draw[PER] = {};
     if (DRAWS && stochastic) {

@@ -1,0 +1,73 @@
+"""AdamW at the ends of fp32: second moments that are subnormal or infinite,
+with an eps that leaves the root alone in the divisor."""
+import numpy as np
+import pytest
+
+import paper_2110_14890_amd as sm
+from gpu_common import require_gpu
+from test_gpu_adamw import as64, snapshot
+from training_common import EPS32, adamw, decode
+
+pytestmark = pytest.mark.gpu
+LEAST = 2.0 ** -149          # fp32's step below 2^-126
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def optimizer(p, by_rows, **kw):
+    return sm.AdamW([p], betas=(0.9, 0.999), weight_decay=0.0, tables=(0,) if by_rows else (), **kw)
+
+
+def step(opt, g, by_rows):
+    """A step of all of a matrix, densely or by its rows, the gradient of
+    every other row as the sum of six entries."""
+    import torch
+    if not by_rows:
+        return opt.step([g])
+    rows = torch.arange(len(g), device=g.device)
+    ids = torch.cat([rows, rows[1::2].repeat(5)]).to(torch.int32)
+    opt.step([sm.row_grad(ids, torch.cat([g, torch.zeros_like(g[1::2]).repeat(5, 1)]))])
+
+
+@pytest.mark.parametrize("by_rows", [False, True])
+@pytest.mark.parametrize("bits,seed", [(32, None), (8, 3), (8, None)])
+@pytest.mark.parametrize("eps", [0.0, 1e-30])
+def test_gradients_whose_squares_are_subnormal(eps, bits, seed, by_rows):
+    """Gradients from 1e-20 to 1e-16, alone and in blocks with ordinary ones:
+    steps of the size of the rate, from each state to the next.
+
+    v is off by three roundings of its terms, each at most 2^-150 where it is
+    subnormal (the square, its product, a decoded root's square) beside the
+    relative ones, so its root is by 2^-149 / v at most, and the step with it;
+    32 half steps hold the rest (the bounds of ordinary steps)."""
+    import torch
+    rng = np.random.default_rng(61)
+    dev = torch.device("cuda")
+    rate, shape = 2e-3, (20, 300)
+    p = torch.zeros(shape, device=dev)
+    opt = optimizer(p, by_rows, lr=rate, eps=eps, bits=bits, seed=seed)
+    scales = ("m_scale", "v_scale")
+    for at in (1, 2, 3):
+        g = 10.0 ** rng.uniform(-20, -16, size=shape) * rng.choice([-1, 1], size=shape)
+        g[5:8, ::7] *= 1e18
+        g = torch.as_tensor(g, dtype=torch.float32, device=dev)
+        p0, s0 = snapshot(p, opt.states[0])
+        step(opt, g, by_rows)
+        m0, v0 = s0["m"].reshape(-1), s0["v"].reshape(-1)
+        if bits == 8:
+            per_row = [np.repeat(s0[k].reshape(20, -1), 128, 1)[:, :300].reshape(-1) if by_rows else None for k in scales]
+            m0, v0 = [decode(x, s0[k]) if r is None else decode(x, np.ones(47)) * r
+                      for x, k, r in zip((m0, v0), scales, per_row)]
+            v0 = v0 ** 2
+        want, _, v = adamw(p0.reshape(-1), as64(g).reshape(-1), m0, v0, rate, (0.9, 0.999), eps, 0.0, at)
+        got = as64(p).reshape(-1)
+        size = np.abs(want - p0.reshape(-1))
+        # the first moment of opposed gradients is a small difference: half steps of its terms
+        terms = rate * 10 * (0.9 * np.abs(m0) + 0.1 * np.abs(as64(g).reshape(-1))) / (np.sqrt(v) / np.sqrt(1 - 0.999 ** at) + eps)
+        assert np.isfinite(got).all(), at
+        assert (np.abs(got - want) <= size * (LEAST / v + 32 * EPS32) + 8 * EPS32 * terms + 4 * EPS32 * np.abs(want)).all(), at
+        if at == 1 and eps == 0.0:
+            assert (np.abs(np.abs(got) / rate - 1) < 0.01).all()
