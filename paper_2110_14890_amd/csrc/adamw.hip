@@ -102,13 +102,13 @@ __host__ __device__ inline uint32_t step_key(uint32_t seed_key, int64_t t)
 // The step's constants for one tensor; false where nothing is to be written.
 // A step's size, rate (m / c1) / (sqrt(v / c2) + eps), as m / -(slope sqrt(v) +
 // floor): one product fewer.  A rate whose reciprocal is not finite stands
-// still.
+// still, whatever v is.
 __host__ __device__ inline void divisor(Step* s, float c1, float c2)
 {
     s->slope = -c1 / (s->rate * sqrtf(c2));
     s->floor = -c1 * s->eps / s->rate;
     if (!(fabsf(s->slope) < INFINITY) || !(fabsf(s->floor) < INFINITY)) {
-        s->slope = 0.0f;
+        s->slope = -1.0f;
         s->floor = -INFINITY;
     }
 }
@@ -146,14 +146,23 @@ __device__ __forceinline__ float root_of(float v)
 }
 // A root of the moments' width.  The hardware's roots take a subnormal number
 // for 0, or here for the least normal one: v of a gradient below 3e-18 in the
-// first step.  Such a v is scaled first; with an eps of that size or 0 the
-// parameter would go to infinity otherwise.
+// first step.  The careful form scales such a v first; with an eps of that
+// size or 0 the parameter would go to infinity otherwise.  It also keeps the
+// root of an infinite v (of a gradient above 1.8e19), which the Newton step
+// makes NaN, and the parameter with it, though by the formula it stands still.
 template <int BITS>
 __device__ __forceinline__ float root(float v)
 {
     return BITS == 8 ? root_of(v) : __builtin_amdgcn_sqrtf(v);
 }
-constexpr int SUBNORMAL = 0x80;   // of v_cmp_class, positive ones
+constexpr int NOT_A_NUMBER = 0x3, SUBNORMAL = 0x80, INFINITE = 0x200;   // of v_cmp_class, positive ones
+template <int BITS>
+__device__ __forceinline__ float careful_root(float v)
+{
+    const bool low = __builtin_amdgcn_classf(v, SUBNORMAL);
+    const float u = root<BITS>(low ? v * 0x1p64f : v) * (low ? 0x1p-32f : 1.0f);
+    return __builtin_amdgcn_classf(v, INFINITE) ? v : u;
+}
 
 __device__ __forceinline__ float first_moment(float m, float g, const Step& s)
 {
@@ -167,6 +176,11 @@ __device__ __forceinline__ float second_moment(float v, float g, const Step& s)
     const float square = g * g;
     const float kept = s.b2 * v, added = s.a2 * square;
     return kept + added;
+}
+
+__device__ __forceinline__ float moved(float p, float m, float u, const Step& s)
+{
+    return fmaf(m, __builtin_amdgcn_rcpf(fmaf(u, s.slope, s.floor)), p * s.keep);
 }
 
 // Codes of four values of [-448, 448].  The stochastic conversion adds its
@@ -309,7 +323,12 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
                                           int64_t block, int j0, float* p, float* g, Held<BITS>& h)
 {
     float m[PER], v[PER], u[PER];
-    bool rare = false;   // a v whose root takes more than the hardware's
+    // A v whose root takes more than the hardware's; for parameters whose lower
+    // bits are rounded off also a NaN, which comes with the gradient or with a
+    // moment before.
+    constexpr bool ROUNDED = sizeof(TP) == 2;
+    constexpr int SPECIAL = SUBNORMAL | (BITS == 8 ? INFINITE : 0) | (ROUNDED ? NOT_A_NUMBER : 0);
+    bool rare = false;
     if (s.scale != 1.0f) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) g[j] *= s.scale;
@@ -337,16 +356,14 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
     for (int j = 0; j < PER; ++j) {
         m[j] = first_moment(m[j], g[j], s);
         v[j] = second_moment(v[j], g[j], s);
+        rare |= __builtin_amdgcn_classf(v[j], SPECIAL);
         u[j] = root<BITS>(v[j]);
-        rare |= __builtin_amdgcn_classf(v[j], SUBNORMAL);
+        p[j] = moved(p[j], m[j], u[j], s);
     }
-    if (__any(rare)) {
+    if (BITS == 32 && ROUNDED && stochastic) {
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (__builtin_amdgcn_classf(v[j], SUBNORMAL)) u[j] = root<BITS>(v[j] * 0x1p64f) * 0x1p-32f;
+        for (int j = 0; j < PER; ++j) rare |= m[j] != m[j];
     }
-#pragma unroll
-    for (int j = 0; j < PER; ++j) p[j] = fmaf(m[j], __builtin_amdgcn_rcpf(fmaf(u[j], s.slope, s.floor)), p[j] * s.keep);
     constexpr bool DRAWS = BITS == 8 || sizeof(TP) == 2;
     uint32_t draw[PER] = {};
     if (DRAWS && stochastic) {
@@ -354,21 +371,19 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
 #pragma unroll
         for (int j = 0; j < PER; ++j) draw[j] = mix(base + (uint32_t)j);
     }
-    uint32_t u_top = 0;   // largest root as bits: NaN above infinity above every number
+    // Once more from the start where a root takes more than the hardware's.  The
+    // branch stands here so that the draws run beside the roots: right behind
+    // them it cost 2 % of the time of 156K rows of 400 and of 320M elements in 8
+    // bits (199.3 against 195.3 us, 615 against 602).
+    if (__any(rare)) {
+        load_floats<TP, PER>((const TP*)t.p + at, have, p);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) u_top = max(u_top, __float_as_uint(u[j]));
-    // Adding to a NaN's lower bits could carry into its sign, and make it 0.
-    // A NaN of that kind comes with the gradient, and makes the root one too,
-    // or with the first moment in 32 bits.
-    bool odd = u_top > 0x7F800000u;
-    if (BITS == 32) {
-#pragma unroll
-        for (int j = 0; j < PER; ++j) odd |= m[j] != m[j];
-    }
-    if (sizeof(TP) == 2 && stochastic && __any(odd)) {
-#pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (p[j] != p[j]) p[j] = __uint_as_float(0x7FC00000u);
+        for (int j = 0; j < PER; ++j) {
+            u[j] = careful_root<BITS>(v[j]);
+            p[j] = moved(p[j], m[j], u[j], s);
+            // adding to a NaN's lower bits could carry into its sign, and make it 0
+            if (ROUNDED && p[j] != p[j]) p[j] = __uint_as_float(0x7FC00000u);
+        }
     }
     if (have > 0) store_params((TP*)t.p + at, have, p, draw, stochastic);
     if constexpr (BITS == 32) {
@@ -380,8 +395,12 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
         // places behind the row's end were loaded as zeros, have no gradient
         // and are 0 still
         float m_top = 0.0f;
+        uint32_t u_top = 0;   // largest root as bits: NaN above infinity above every number
 #pragma unroll
-        for (int j = 0; j < PER; ++j) m_top = fmaxf(m_top, fabsf(m[j]));
+        for (int j = 0; j < PER; ++j) {
+            m_top = fmaxf(m_top, fabsf(m[j]));
+            u_top = max(u_top, __float_as_uint(u[j]));
+        }
         u_top = block_max(u_top);
         m_top = __uint_as_float(block_max(__float_as_uint(m_top)));
         // a moment that is not finite, now or before, makes both NaN

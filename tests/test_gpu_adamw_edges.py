@@ -71,3 +71,40 @@ def test_gradients_whose_squares_are_subnormal(eps, bits, seed, by_rows):
         assert (np.abs(got - want) <= size * (LEAST / v + 32 * EPS32) + 8 * EPS32 * terms + 4 * EPS32 * np.abs(want)).all(), at
         if at == 1 and eps == 0.0:
             assert (np.abs(np.abs(got) / rate - 1) < 0.01).all()
+
+
+@pytest.mark.parametrize("by_rows", [False, True])
+@pytest.mark.parametrize("rate", [2e-3, 0.0])
+@pytest.mark.parametrize("bits,seed", [(32, None), (8, 3)])
+def test_second_moments_that_are_infinite(bits, seed, rate, by_rows):
+    """A gradient whose square is no fp32 number: the parameter stands still
+    (a finite moment over an infinite root) in either width, and its
+    neighbours take their ordinary step.  The moments of its block are lost in
+    8 bits from then on, and the block's parameters NaN in the step after."""
+    import torch
+    dev = torch.device("cuda")
+    p = torch.ones((4, 300), device=dev)
+    opt = optimizer(p, by_rows, lr=rate, bits=bits, seed=seed)
+    g = torch.full((4, 300), 0.5, device=dev)
+    g[1, 7], g[2, 290] = 1e20, -1e25
+    step(opt, g, by_rows)
+    # a first step is the rate times the gradient's sign: 1 less 16 half steps of the rate and 2 of 1
+    got, moved = as64(p), np.ones((4, 300), bool)
+    moved[1, 7] = moved[2, 290] = False
+    assert (got[~moved] == 1.0).all()
+    assert (np.abs(got[moved] - (1.0 - np.float32(rate))) <= 16 * EPS32 * rate + 2 * EPS32).all()
+    if bits == 32:
+        assert torch.isinf(opt.states[0]["v"]).nonzero().tolist() == [[1, 7], [2, 290]]
+    # in 8 bits blocks of 128 elements of a row, or of the whole matrix
+    lost = ~moved
+    if bits == 8:
+        block = np.arange(300) // 128 + 3 * np.arange(4)[:, None] if by_rows else np.arange(1200).reshape(4, 300) // 128
+        lost = np.isin(block, block[~moved])
+        assert np.isnan(as64(opt.states[0]["m_scale"])).sum() == np.isnan(as64(opt.states[0]["v_scale"])).sum() == 2
+    step(opt, torch.full((4, 300), 0.5, device=dev), by_rows)
+    got = as64(p)
+    if bits == 8:
+        assert np.isnan(got[lost]).all()
+    else:
+        assert (got[lost] == 1.0).all()
+    assert (np.abs(got[~lost] - (1.0 - 2 * rate)) <= 2 * (16 * EPS32 * rate + 2 * EPS32) + 2.0 ** -3 * rate * (bits == 8)).all()
