@@ -418,8 +418,9 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
             u[j] = y;
         }
         // a root that is not 0 has a code that is not 0 (rarely below it: a
-        // root under 2^-18 of its block's largest)
-        if (__any(least < LEAST_CODE)) {
+        // root under 2^-18 of its block's largest; lanes without a column hold
+        // roots that are 0, which need nothing)
+        if (__any(have > 0 && least < LEAST_CODE)) {
 #pragma unroll
             for (int j = 0; j < PER; ++j)
                 if (p[j] != 0.0f && u_unit > 0.0f) u[j] = fmaxf(u[j], LEAST_CODE);
@@ -582,6 +583,13 @@ struct RowSum {
 #pragma unroll
             for (int j = 0; j < PER; ++j) g[j] += __shfl_xor(g[j], d);
         }
+        // Fewer than 16 lanes hold a row of at most 64 columns: the other lanes
+        // of its block own no column, and a copy of another lane's sum must not
+        // count in the block's largest moment.
+        if (MOST == 16 && (int)(threadIdx.x & 63) >= lanes) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) g[j] = 0.0;
+        }
     }
 };
 
@@ -649,12 +657,14 @@ struct LongRun {
 // Rows that LANES lanes hold (16 or 32: up to 128 or 256 columns) are stepped
 // 64 / LANES at a time, where their runs are short; wider ones that one chunk
 // holds two at a time; the others one by one.
+// Narrow rows with 8-bit moments are held to the registers of five wavefronts
+// a SIMD: 264K entries of 192K rows of 100 columns 88 us, with four 96.
 // 156K rows of 400 (264K entries), 8-bit moments: 194 us; 14.4K rows (66K
 // entries) in 32 bits: 37 us, 3.7 TB/s.  The first is bound by the vector
 // operations of k_adamw in 50 of 64 lanes, the second by the MALL.
 constexpr int SHORT = 4;
 template <class TP, class TG, int BITS, int LANES>
-__global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyper hyper, int window)
+__global__ __launch_bounds__(64, LANES < 64 && BITS == 8 ? 5 : 1) void k_adamw_rows(const RowsTensor r, const Hyper hyper, int window)
 {
     const int lane = threadIdx.x;
     const int64_t first = (int64_t)blockIdx.x * window;   // lane 1 looks at this entry
@@ -783,11 +793,8 @@ __global__ __launch_bounds__(64) void k_adamw_rows(const RowsTensor r, const Hyp
                     sum.entries(run.tail, run.end);
                 }
                 sum.finish();
-                // Rows of at most 64 columns are summed by groups of fewer than 16
-                // lanes: what a lane without a column has of it is another lane's,
-                // and must not count in their block's largest moment.
 #pragma unroll
-                for (int j = 0; j < PER; ++j) g[j] = have > 0 ? (float)sum.g[j] : 0.0f;
+                for (int j = 0; j < PER; ++j) g[j] = (float)sum.g[j];
             }
             load_floats<TP, PER>((const TP*)r.t.p + at, have, p);
             load_held<BITS>(r.t, at, have, block, h);
