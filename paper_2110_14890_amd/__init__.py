@@ -766,7 +766,8 @@ class RowGrad:
     rows (int32, ascending, repeats allowed) adds coef[o] times
     grad[o // per], o = order[i], to its row (order int64 and coef fp32 by
     entry, both optional).  Entries outside the table are skipped.  With
-    in_order False the rows may be in any order (order None): AdamW sorts them."""
+    in_order False the rows may be in any order, and rows and coef of any shape
+    and strides (order None): AdamW flattens and sorts them, on its stream."""
 
     def __init__(self, rows, grad, order=None, coef=None, per: int = 1, in_order: bool = True):
         self.rows, self.grad, self.order, self.coef, self.per, self.in_order = rows, grad, order, coef, per, in_order
@@ -776,8 +777,9 @@ def row_grad(ids, grad, coef=None, per: int = 1) -> RowGrad:
     """RowGrad of ids in any order and shape (int32): entry i, counted over
     the flattened ids, adds coef[i] times grad[i // per].  With score()'s
     candidates [batch, n] as ids, its queries as grad, the gradient of its
-    scores as coef and per = n this is score()'s gradient for the table."""
-    return RowGrad(ids.reshape(-1), grad, None, None if coef is None else coef.reshape(-1), per, in_order=False)
+    scores as coef and per = n this is score()'s gradient for the table.
+    Nothing is launched before the step."""
+    return RowGrad(ids, grad, None, coef, per, in_order=False)
 
 
 def sort_rows(ids, n_rows: int, stream=None):
@@ -992,28 +994,40 @@ class AdamW:
         if p.dim() != 2 or not self._by_rows[k]:
             raise ValueError(f"parameter {k} is no table with moments per row: its gradient cannot be a RowGrad")
         n = g.rows.numel()
-        ok = lambda t, dtype, numel: t.dtype == dtype and t.device == self.device and t.is_contiguous() and t.numel() == numel
-        if not ok(g.rows, torch.int32, n):
-            raise ValueError(f"rows of gradient {k} must be a contiguous int32 tensor on {self.device}")
-        if g.order is not None and not ok(g.order, torch.int64, n):
+        rows, order, coef = g.rows, g.order, g.coef
+        ok = lambda t, dtype, numel: t.dtype == dtype and t.device == self.device and t.numel() == numel and \
+            (t.is_contiguous() or not g.in_order)
+        of = "contiguous " if g.in_order else ""
+        if not ok(rows, torch.int32, n):
+            raise ValueError(f"rows of gradient {k} must be a {of}int32 tensor on {self.device}")
+        if order is not None and not ok(order, torch.int64, n):
             raise ValueError(f"order of gradient {k} must be a contiguous int64 tensor of {n} entries on {self.device}")
-        if g.coef is not None and not ok(g.coef, torch.float32, n):
-            raise ValueError(f"coef of gradient {k} must be a contiguous fp32 tensor of {n} entries on {self.device}")
+        if coef is not None and not ok(coef, torch.float32, n):
+            raise ValueError(f"coef of gradient {k} must be a {of}fp32 tensor of {n} entries on {self.device}")
         if g.per < 1 or g.grad.dim() != 2 or g.grad.shape[1] != p.shape[1] or g.grad.shape[0] * g.per < n or \
                 g.grad.dtype not in _TYPES or g.grad.device != self.device or not g.grad.is_contiguous():
             raise ValueError(f"gradient {k} must hold contiguous rows of {p.shape[1]} on {self.device}, one for each "
                              f"{g.per} of {n} entries, got {g.grad.dtype} {tuple(g.grad.shape)} on {g.grad.device}")
-        if not g.in_order and g.order is not None:
+        if not g.in_order and order is not None:
             raise ValueError(f"gradient {k} has an order, but its rows are not in order")
         if n == 0:
             return False
-        rows, order = (g.rows, g.order) if g.in_order else sort_rows(g.rows, p.shape[0], stream)
-        kept.append((rows, order))
-        if stream is not None:      # what row_grad made may be freed before that stream gets here
+        if not g.in_order:
+            # copies of what is not contiguous belong on the step's stream: a copy on the
+            # current one would come behind what that stream was made to wait for
+            flat = lambda: [t if t is None else t.reshape(-1) for t in (rows, coef)]
+            if stream is None:
+                rows, coef = flat()
+            else:
+                with torch.cuda.stream(stream):
+                    rows, coef = flat()
+            rows, order = sort_rows(rows, p.shape[0], stream)
+        kept.append((rows, order, coef))
+        if stream is not None:      # the caller's may be freed before that stream gets here
             for t in (g.rows, g.grad, g.order, g.coef):
                 if t is not None:
                     t.record_stream(stream)
         x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), _TYPES[g.grad.dtype], rows.data_ptr(), \
-            None if order is None else order.data_ptr(), None if g.coef is None else g.coef.data_ptr()
+            None if order is None else order.data_ptr(), None if coef is None else coef.data_ptr()
         x.n_entries, x.per, self._last[k] = n, g.per, RowGrad
         return True
