@@ -509,6 +509,12 @@ def gather_probe(table, n_reads: int, stream=None):
 # autograd does not see the calls (torch.autograd.backward(queries,
 # score_grad(...)) goes on into a model's own graph).
 #
+# A call's stream is the device's current one, or the one given as stream.  The
+# caller makes a given stream wait for what made the inputs, and waits for it
+# before using the outputs, which belong to that stream.  Inputs and outputs
+# may be let go of as soon as the call returns: their memory is kept until the
+# stream has got there.
+#
 # Small calls take as long as this binding does, so the checks of a call are
 # plain comparisons; what is wrong is spelled out only where one fails.
 _torch = None
@@ -537,10 +543,11 @@ def _lazy_torch():
     return _torch
 
 
-def _launch(device, stream, call):
+def _launch(device, stream, call, uses=()):
     """call(stream handle) with the device current and its stream: the given
     one, or the device's current stream.  Tensors that call makes belong to
-    that stream."""
+    that stream; of a given one, the tensors of uses are not given back to the
+    allocator before it has got there."""
     torch = _torch
     if device.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, not on {device}")
@@ -548,7 +555,11 @@ def _launch(device, stream, call):
         if stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
         with torch.cuda.stream(stream):
-            return call(stream.cuda_stream)
+            result = call(stream.cuda_stream)
+        for t in uses:
+            if t is not None:
+                t.record_stream(stream)
+        return result
     if torch.cuda.current_device() == device.index:
         return call(torch._C._cuda_getCurrentRawStream(device.index))
     with torch.cuda.device(device):
@@ -612,7 +623,7 @@ def score_into(table, queries, candidates, scores, stream=None):
     _lazy_torch()
     args = _score_args(table, candidates, queries, "queries", scores, "scores")
     _check(_launch(table.device, stream, lambda st: lib().smore_score(
-        args, _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st)))
+        args, _ptr(table), _ptr(queries), _ptr(candidates), _ptr(scores), st), (table, queries, candidates, scores)))
     return scores
 
 
@@ -621,7 +632,12 @@ def score(table, queries, candidates, stream=None):
     sampled): the product of queries [batch, dim] with the candidates' rows of
     table [V, dim], 0 for candidates outside [0, V) (smore_score).  For one
     candidate set shared by all queries, candidates.expand(batch, n) works,
-    but a matrix product with the set's rows is the faster way."""
+    but a matrix product with the set's rows is the faster way.
+
+    stream: a torch.cuda.Stream to run on instead of the current one.  The
+    caller makes it wait for what made the inputs, and waits for it before
+    using the scores; the inputs may be let go of at once.  The same holds for
+    the other training calls."""
     torch = _lazy_torch()
     new = lambda _: torch.empty(candidates.shape, dtype=torch.float32, device=table.device)
     scores = new(None) if stream is None else _launch(table.device, stream, new)
@@ -642,7 +658,7 @@ def score_grad_into(table, candidates, grad_scores, grad_queries, stream=None):
         return L.smore_score_grad(args, _ptr(table), _ptr(candidates), _ptr(grad_scores),
                                   _ptr(grad_queries), _ptr(ws), need, st)
 
-    _check(_launch(table.device, stream, call))
+    _check(_launch(table.device, stream, call, (table, candidates, grad_scores, grad_queries)))
     return grad_queries
 
 
@@ -717,13 +733,14 @@ def _preference(positive, negatives, out, ref_positive, ref_negatives, n_valid, 
                           {"n_valid": n_valid, "mask": mask, "weight": weight, "loss": loss})
     at = lambda t: 0 if t is None else t.data_ptr()
     step = lambda t: 0 if t is None else t.stride(0)
+    uses = (positive, negatives, ref_positive, ref_negatives, n_valid, mask, weight, loss, grad_p, grad_n)
     if n == 0:
         negatives = ref_negatives = grad_n = mask = None
     args = _pack_preference(batch, n, number, _TYPES[dtype], beta, smoothing, scale, positive.stride(0), step(negatives),
                             step(ref_positive), step(ref_negatives), step(grad_p), step(grad_n))
     ins = _pack_in(positive.data_ptr(), at(negatives), at(ref_positive), at(ref_negatives), at(n_valid), at(mask), at(weight))
     outs = _pack_out(at(loss), at(grad_p), at(grad_n))
-    _check(_launch(device, stream, lambda st: lib().smore_preference_loss(args, ins, outs, st)))
+    _check(_launch(device, stream, lambda st: lib().smore_preference_loss(args, ins, outs, st), uses))
     return out
 
 
@@ -798,7 +815,7 @@ def sort_rows(ids, n_rows: int, stream=None):
         _check(L.smore_sort_rows(_ptr(ids), n, n_rows, _ptr(rows), _ptr(order), _ptr(ws), size.value, st))
         return rows, order
 
-    return _launch(ids.device, stream, call)
+    return _launch(ids.device, stream, call, (ids,))
 
 
 def alloc_adamw_state(param, bits: int = 32, table: bool = False) -> dict:
@@ -922,7 +939,7 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        used, device, scaled, tables, sorts = [], self.device, self.bits == 8, False, []
+        used, device, scaled, tables, kept = [], self.device, self.bits == 8, False, []
         if self.weight_decay != self._decays:
             self._take_decays()
         for k, g in enumerate(grads):
@@ -936,7 +953,7 @@ class AdamW:
                     (scaled and (state["m_scale"].data_ptr() != seen[5] or state["v_scale"].data_ptr() != seen[6])):
                 self._describe(k)
             if type(g) is RowGrad:
-                if not self._rows(k, self._items[k], p, g, stream, sorts):
+                if not self._rows(k, self._items[k], p, g, stream, kept):
                     continue
                 tables = True
             else:
@@ -981,7 +998,13 @@ class AdamW:
                 self.device_steps.sub_(1)
             return rc
 
-        _check(_launch(device, stream, call))
+        if stream is not None:
+            kept += [grad_scale, self.lr if device_lr else None, self.device_steps]
+            for k in used:
+                kept += [self.params[k], *self.states[k].values()]
+                if type(grads[k]) is not RowGrad:
+                    kept.append(grads[k])
+        _check(_launch(device, stream, call, kept))
         self.steps += 1
         # autograd sees that they changed
         torch.autograd.graph.increment_version([p for p in (self.params[k] for k in used) if not p.is_inference()])
@@ -1022,11 +1045,7 @@ class AdamW:
                 with torch.cuda.stream(stream):
                     rows, coef = flat()
             rows, order = sort_rows(rows, p.shape[0], stream)
-        kept.append((rows, order, coef))
-        if stream is not None:      # the caller's may be freed before that stream gets here
-            for t in (g.rows, g.grad, g.order, g.coef):
-                if t is not None:
-                    t.record_stream(stream)
+        kept.extend((rows, order, coef, g.rows, g.grad, g.order, g.coef))
         x.grad, x.grad_type, x.rows, x.order, x.coef = g.grad.data_ptr(), _TYPES[g.grad.dtype], rows.data_ptr(), \
             None if order is None else order.data_ptr(), None if coef is None else coef.data_ptr()
         x.n_entries, x.per, self._last[k] = n, g.per, RowGrad
