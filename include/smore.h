@@ -485,7 +485,10 @@ int smore_sort_rows(const int32_t *ids, int64_t n, int32_t n_rows, int32_t *rows
    SMORE_ADAMW_STOCHASTIC: codes and bf16 parameters are rounded up or down
    at random by their remainder (nearest, ties to even, without it), from a
    hash of (seed, t, index, position): a step that is run again from the same
-   values gives the same bits.  index tells the tensors of a model apart. */
+   values gives the same bits.  index tells the tensors of a model apart.
+   Moments in 8 bits need it: a step changes v by 1 - beta2 of itself, a code is
+   1/16 to 1/8 of its value wide, so rounded to the nearest a code stays where
+   it is whatever the gradients do. */
 #define SMORE_ADAMW_BLOCK 128
 #define SMORE_ADAMW_STOCHASTIC 1u
 

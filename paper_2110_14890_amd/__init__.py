@@ -845,8 +845,11 @@ class AdamW:
     tables: numbers of the parameters that are tables [V, dim] stepped by
     rows (RowGrad).  states: their moments as alloc_adamw_state makes them,
     e.g. of a checkpoint (they are used, not copied), steps the steps taken.
-    seed: roundings to 8 bits and to bf16 are stochastic, keyed by it (None:
-    to the nearest).  lr: a number, or an fp32 device tensor [1].  device_step:
+    seed: roundings to 8 bits and to bf16 are stochastic, keyed by it; None
+    rounds to the nearest, with which moments in 8 bits hardly move once they
+    have a code (a step changes v by 1 - beta2 of itself, a code is 1/16 to 1/8
+    wide): for comparisons only.  "default" is 0 with moments in 8 bits, None
+    with 32.  lr: a number, or an fp32 device tensor [1].  device_step:
     the step count is kept in an int64 device tensor, counted up by a kernel,
     so that a captured step counts when it is replayed.
 
@@ -854,10 +857,12 @@ class AdamW:
     .eps and .weight_decay may be changed between steps."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
-                 bits: int = 32, seed: "int | None" = None, tables=(), states=None, steps: int = 0,
+                 bits: int = 32, seed: "int | str | None" = "default", tables=(), states=None, steps: int = 0,
                  device_step: bool = False):
         torch = _lazy_torch()
         self.params = list(params)
+        if seed == "default":
+            seed = 0 if bits == 8 else None
         self.lr, self.betas, self.eps, self.seed, self.steps = lr, betas, eps, seed, steps
         self.weight_decay, self._decays = self._decay_list(weight_decay), None
         if not self.params:

@@ -108,3 +108,59 @@ def test_second_moments_that_are_infinite(bits, seed, rate, by_rows):
     else:
         assert (got[lost] == 1.0).all()
     assert (np.abs(got[~lost] - (1.0 - 2 * rate)) <= 2 * (16 * EPS32 * rate + 2 * EPS32) + 2.0 ** -3 * rate * (bits == 8)).all()
+
+
+def test_eight_bit_moments_follow_the_gradients_by_default():
+    """sqrt(v) after the gradients grew from 0.05 to 0.4, one element of each
+    block as large as that all the time, so that the scales stay.
+
+    A root u is rounded by a code's step s <= u / 8 at most, up or down with
+    mean 0, and returns to its value at a rate of 1 - b2 a step.  Rounded
+    that way an element's variance gains (distance to the value) x (1 - b2) s
+    and loses 2 (1 - b2) of itself a step, so its spread is at most s / 2, a
+    sixteenth.  Of 4,064 independent elements the mean is then within
+    5 / 16 / sqrt(4,064) = 0.5 %; that sqrt(b2 u^2 + ..) is convex adds half
+    the variance, 0.2 %, and 0.5 % is left for the elements' finite number of
+    codes.  Rounded to the nearest u would stay near 0.05."""
+    import torch
+    dev = torch.device("cuda")
+    b2, size = 0.999, 4096
+    p = torch.zeros(size, device=dev)
+    opt = sm.AdamW([p], lr=1e-6, betas=(0.9, b2), weight_decay=0.0, bits=8)
+    assert opt.seed is not None
+    small, large = torch.full((size,), 0.05, device=dev), torch.full((size,), 0.4, device=dev)
+    small[::128] = 0.4
+    for _ in range(3000):
+        opt.step([small])
+    for _ in range(8000):
+        opt.step([large])
+    s = opt.states[0]
+    u = decode(as64(s["v"]), as64(s["v_scale"]))
+    want = np.sqrt((1 - b2 ** 8000) * 0.4 ** 2 + b2 ** 8000 * (1 - b2 ** 3000) * 0.05 ** 2)
+    moved = np.arange(size) % 128 != 0
+    assert abs(u[moved].mean() / want - 1) < 0.012
+    assert abs((u[moved] ** 2).mean() / want ** 2 - 1) < 0.03
+    assert u.min() > 0.5 * want and u.max() < 1.6 * want      # eight and ten spreads
+
+
+def test_the_default_seed():
+    """0 with moments in 8 bits; none with 32, where parameters in bf16 are
+    rounded to the nearest.  A seed that is given is taken."""
+    import torch
+    rng = np.random.default_rng(62)
+    dev = torch.device("cuda")
+    start = torch.as_tensor(rng.normal(size=3000), dtype=torch.bfloat16, device=dev)
+    grads = [torch.as_tensor(rng.normal(size=3000), dtype=torch.float32, device=dev) for _ in range(3)]
+
+    def run(**kw):
+        p = start.clone()
+        opt = sm.AdamW([p], lr=1e-2, **kw)
+        for g in grads:
+            opt.step([g])
+        return p, opt.states[0]["v"].view(torch.uint8).clone()
+
+    same = lambda a, b: all(torch.equal(x, y) for x, y in zip(a, b))
+    assert same(run(bits=8), run(bits=8, seed=0)) and same(run(bits=32), run(bits=32, seed=None))
+    for other in (None, 1):
+        assert not same(run(bits=8), run(bits=8, seed=other))
+    assert not same(run(bits=32), run(bits=32, seed=0))
