@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+import weakref
 
 import numpy as np
 
@@ -931,7 +932,11 @@ class AdamW:
         x.m_scale, x.v_scale = (state["m_scale"].data_ptr(), state["v_scale"].data_ptr()) if self.bits == 8 else (None, None)
         x.n_rows, x.dim = (p.shape[0], p.shape[1]) if p.dim() == 2 else (1, p.numel())
         x.param_type, x.bits, x.index = _TYPES[p.dtype], self.bits, k
-        self._seen[k] = [p.shape, p] + [t.data_ptr() for t in (p, *(state[n] for n in shapes))]
+        moments = [state[n] for n in shapes]
+        at = [t.data_ptr() for t in (p, *moments)]
+        # a moment that goes away leaves its address to others: what was found out here ends with it
+        ended = lambda _: at.__setitem__(0, None)
+        self._seen[k] = (p.shape, p, p.dtype, at, [weakref.ref(t, ended) for t in moments])
         self._by_rows[k], self._whole[k], self._last[k], self._empty[k] = by_rows, whole, None, p.numel() == 0
 
     def step(self, grads, grad_scale=None, stream=None) -> None:
@@ -953,9 +958,10 @@ class AdamW:
             p, state, seen = self.params[k], self.states[k], self._seen[k]
             shape = p.shape
             # a parameter or moments that were replaced are looked at again
-            if p is not seen[1] or shape != seen[0] or not p.is_contiguous() or p.data_ptr() != seen[2] \
-                    or state["m"].data_ptr() != seen[3] or state["v"].data_ptr() != seen[4] or \
-                    (scaled and (state["m_scale"].data_ptr() != seen[5] or state["v_scale"].data_ptr() != seen[6])):
+            at = seen[3]
+            if p is not seen[1] or shape != seen[0] or p.dtype is not seen[2] or not p.is_contiguous() \
+                    or p.data_ptr() != at[0] or state["m"].data_ptr() != at[1] or state["v"].data_ptr() != at[2] or \
+                    (scaled and (state["m_scale"].data_ptr() != at[3] or state["v_scale"].data_ptr() != at[4])):
                 self._describe(k)
             if type(g) is RowGrad:
                 if not self._rows(k, self._items[k], p, g, stream, kept):

@@ -164,3 +164,68 @@ def test_the_default_seed():
     for other in (None, 1):
         assert not same(run(bits=8), run(bits=8, seed=other))
     assert not same(run(bits=32), run(bits=32, seed=0))
+
+
+@pytest.mark.parametrize("bits,name", [(32, "m"), (32, "v"), (8, "m"), (8, "v"), (8, "m_scale"), (8, "v_scale")])
+def test_moments_replaced_at_the_same_address(bits, name):
+    """A state's tensor that was let go of, and a smaller one or one of another
+    type in its place (which the allocator puts at the same address): looked
+    at again, and refused."""
+    import torch
+    dev = torch.device("cuda")
+    p = torch.ones(12800, device=dev)
+    opt = sm.AdamW([p], lr=1e-3, bits=bits)
+    g = torch.ones(12800, device=dev)
+    opt.step([g])
+    state = opt.states[0]
+    whole = state[name].numel()
+    for count, dtype in ((whole - 1, state[name].dtype), (whole * state[name].element_size() // 2, torch.float16)):
+        shape = state[name].shape
+        torch.cuda.synchronize()
+        state[name] = None
+        state[name] = torch.zeros(count, dtype=torch.uint8, device=dev).view(dtype) if dtype == torch.float8_e4m3fn else \
+            torch.zeros(count, dtype=dtype, device=dev)
+        with pytest.raises(ValueError, match="m_scale|fits"):
+            opt.step([g])
+        state[name] = torch.zeros(shape, dtype=torch.float32 if bits == 32 or "scale" in name else torch.uint8, device=dev)
+        if bits == 8 and "scale" not in name:
+            state[name] = state[name].view(torch.float8_e4m3fn)
+        opt.step([g])
+    assert torch.isfinite(p).all() and opt.steps == 3
+
+
+def test_a_parameter_of_another_type_at_the_same_address():
+    """A parameter's data replaced twice: its type is looked at, not only where
+    it lies."""
+    import torch
+    dev = torch.device("cuda")
+    p = torch.ones(12800, device=dev)
+    opt = sm.AdamW([p], lr=0.5, weight_decay=0.0)
+    g = torch.ones(12800, device=dev)
+    opt.step([g])
+    p.data = p.data.double()
+    p.data = p.data.to(torch.bfloat16)
+    opt.step([g])
+    # two steps of 0.5, each off by 16 half steps of itself at most (the bound of ordinary steps): the first leaves
+    # 0.5 (1 - 2^-20) to 0.5 (1 + 2^-20), which is 0.5 in bf16, the second 8 half steps of 1 beside 0, and the sum's own
+    assert p.dtype == torch.bfloat16 and (p.abs() <= 10 * EPS32).all()
+    p.data = p.data.double()
+    with pytest.raises(ValueError, match="fp32 or bf16"):
+        opt.step([g])
+
+
+def test_an_optimizer_that_is_let_go_of_frees_its_tensors():
+    import gc
+    import weakref
+
+    import torch
+    p = torch.ones(300, device="cuda")
+    opt = sm.AdamW([p], lr=0.5, bits=8)
+    opt.step([torch.ones(300, device="cuda")])
+    gone = [weakref.ref(t) for t in (p, *opt.states[0].values())]
+    gc.disable()
+    try:
+        del p, opt
+        assert all(r() is None for r in gone)
+    finally:
+        gc.enable()
