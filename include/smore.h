@@ -435,8 +435,10 @@ typedef struct {
    (both NULL: not wanted).  A row without a valid negative has loss and
    gradients 0; places that are not valid are not used and get gradient 0.
    A valid score that is NaN makes its row NaN, as in the formula, and so does
-   a negative at +infinity with SMORE_PREFERENCE_SOFTMAX.  Outputs must not
-   overlap inputs or each other. */
+   a z_k of -infinity (a negative at +infinity, a positive at -infinity) with
+   SMORE_PREFERENCE_SOFTMAX; with SMORE_PREFERENCE_PAIRS a row's loss is infinite
+   where the sum over its negatives passes fp32.  Outputs must not overlap inputs
+   or each other. */
 typedef struct {
     float *loss;
     void *grad_positive, *grad_negatives;

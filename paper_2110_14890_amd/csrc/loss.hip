@@ -167,9 +167,9 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
             if (GRAD) ((T*)a.grad_pos)[b * a.grad_pos_stride] = (T)slopes;
         }
     } else {
-        // exponents to the base 2; running maximum (of 0, the positive's own
-        // term, on) and sum of each lane
-        const float rate = a.beta * LOG2E;
+        // running maximum of -z (of 0, the positive's own term, on) and sum of
+        // each lane.  The base's factor comes behind the difference: in front of
+        // it a -z above 2.3e38 (a positive at its type's lowest value) overflows.
         float top = 0.0f, sum = 0.0f;
         float e[STEPS][V];
         auto exponents = [&](int at0) {
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int j = 0; j < V; ++j) e[s][j] = rate * d[s][j];
+                for (int j = 0; j < V; ++j) e[s][j] = a.beta * d[s][j];
             if (!full) {
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s)
@@ -195,22 +195,22 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
                 for (int j = 0; j < V; ++j) m = fmaxf(m, e[s][j]);
-            sum *= __builtin_amdgcn_exp2f(top - m);
+            sum *= __builtin_amdgcn_exp2f(LOG2E * (top - m));
             top = m;
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    e[s][j] = __builtin_amdgcn_exp2f(e[s][j] - top);
+                    e[s][j] = __builtin_amdgcn_exp2f(LOG2E * (e[s][j] - top));
                     sum += e[s][j];
                 }
         }
         float high = across<WAVES>(max64(top), lds, wave, [](float x, float y) { return fmaxf(x, y); });
-        const float mine = __builtin_amdgcn_exp2f(top - high);
+        const float mine = __builtin_amdgcn_exp2f(LOG2E * (top - high));
         sum = across<WAVES>(sum64(sum * mine), lds, wave, [](float x, float y) { return x + y; });
-        const float total = __builtin_amdgcn_exp2f(-high) + sum;
+        const float total = __builtin_amdgcn_exp2f(-LOG2E * high) + sum;
         if (lane == 0 && wave == 0) {
-            if (a.loss) a.loss[b] = high > 0.0f ? fmaf(high, LN2, __logf(total)) : log1pf(sum);
+            if (a.loss) a.loss[b] = high > 0.0f ? high + __logf(total) : log1pf(sum);
             if (GRAD) ((T*)a.grad_pos)[b * a.grad_pos_stride] = (T)(sum == 0.0f ? 0.0f : -gain * (sum / total));
         }
         if constexpr (GRAD) {
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
 #pragma unroll
                     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                        for (int j = 0; j < V; ++j) e[s][j] = __builtin_amdgcn_exp2f(e[s][j] - top);
+                        for (int j = 0; j < V; ++j) e[s][j] = __builtin_amdgcn_exp2f(LOG2E * (e[s][j] - top));
                 }
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
