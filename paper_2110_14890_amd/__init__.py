@@ -507,8 +507,8 @@ def gather_probe(table, n_reads: int, stream=None):
 
 # ------------------------------------------------- training on sampled batches
 # Gradients are outputs and inputs of these calls, as the C ABI has them:
-# autograd does not see the calls (torch.autograd.backward(queries,
-# score_grad(...)) goes on into a model's own graph).
+# autograd does not see the calls (queries.backward(score_grad(...)) goes on
+# into a model's own graph).
 #
 # A call's stream is the device's current one, or the one given as stream.  The
 # caller makes a given stream wait for what made the inputs, and waits for it
@@ -635,6 +635,10 @@ def score(table, queries, candidates, stream=None):
     candidate set shared by all queries, candidates.expand(batch, n) works,
     but a matrix product with the set's rows is the faster way.
 
+    Autograd does not see the call, whether or not its inputs require
+    gradients: the scores have no history.  Their gradients are score_grad()
+    for the queries and row_grad() for the table.
+
     stream: a torch.cuda.Stream to run on instead of the current one.  The
     caller makes it wait for what made the inputs, and waits for it before
     using the scores; the inputs may be let go of at once.  The same holds for
@@ -666,7 +670,9 @@ def score_grad_into(table, candidates, grad_scores, grad_queries, stream=None):
 def score_grad(table, candidates, grad_scores, dtype=None, stream=None):
     """Gradient of score() for the queries, [batch, dim] in dtype (fp32): the
     sum of the candidates' rows, each times its entry of grad_scores (fp32
-    [batch, n]).  The gradient for the table is AdamW's: row_grad()."""
+    [batch, n]).  The gradient for the table is AdamW's: row_grad().  Nothing is
+    accumulated into .grad; queries.backward(score_grad(...)) goes on into the
+    graph that the queries came from."""
     torch = _lazy_torch()
     new = lambda _: torch.empty((candidates.shape[0], table.shape[1]), dtype=dtype or torch.float32, device=table.device)
     out = new(None) if stream is None else _launch(table.device, stream, new)
@@ -757,7 +763,9 @@ def preference_loss(positive, negatives, ref_positive=None, ref_negatives=None, 
     "pairs" averages the paired losses, with label smoothing; "softmax"
     takes the positive against all negatives at once.  The formulas stand at
     smore_preference_loss.  Scores may be views of one matrix (a column, the
-    columns behind it)."""
+    columns behind it).  Autograd does not see the call: the loss has no
+    history, and loss.backward() is not the way to the gradients, which are
+    outputs."""
     torch = _lazy_torch()
 
     def new(_):
