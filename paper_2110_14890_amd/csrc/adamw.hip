@@ -17,6 +17,10 @@
 // probability of the remainder, which is right in the mean.  A sqrt(v) that
 // is not 0 never gets the code 0, so that no later step divides by eps alone.
 // A moment that is not finite makes the scales of its 128 elements NaN.
+// Unbiased for m and sqrt(v), that is; v, their square, settles 5 % high under
+// Gaussian gradients, half to twice its value at the 1st and 99th percentiles
+// (262,144 elements, 10,000 steps, b2 = 0.999; to the nearest 23 % high, and
+// hardly to be moved from there).
 // Parameters in bf16 are rounded the same way.  The random bits are a hash
 // of (seed, step, tensor, block, element): nothing is kept between calls.
 #include <hip/hip_runtime.h>
@@ -47,7 +51,7 @@ struct Step {
 };
 
 struct Hyper {
-    Step s;                             // as the host knows it (keep for decay 0)
+    Step s;                             // as the host knows it (without keep, a tensor's)
     float c1, c2, log_b1, log_b2;       // c = 1 - b^t
     const int64_t* step;                // step, rate and gradient scale on the device, or NULL
     const float* lr_dev;
@@ -85,6 +89,8 @@ struct RowsTensor {
     uint32_t per;
 };
 
+// A published hash of 32-bit words: C. Wellons' lowbias32 (2018), two rounds of
+// a shift and a product whose constants were searched for the least bias.
 __host__ __device__ inline uint32_t mix(uint32_t x)
 {
     x ^= x >> 16;
@@ -236,8 +242,10 @@ __device__ __forceinline__ void block_scale(float top, bool lost, float* scale, 
     *unit = some ? fmaf(fmaf(-top, r, 1.0f), r, r) * 448.0f : 0.0f;
 }
 
-// A lane's parameters to memory; bf16 rounded stochastically by bits that are
-// a product's of the element's draw.
+// A lane's parameters to memory; bf16 rounded stochastically by the upper half
+// of a product of the element's draw: by 2^32 over the golden ratio
+// (multiplicative hashing, Knuth), after an exclusive or with a constant of
+// MurmurHash3's (A. Appleby), so that a draw of 0 has bits too.
 __device__ __forceinline__ void store_params(float* dst, int have, const float* p, const uint32_t*, bool)
 {
     store_floats<float, PER>(dst, have, p);
@@ -511,8 +519,10 @@ __device__ __forceinline__ Entry entry_of(const RowsTensor& r, int64_t at, int64
     return entry_at(r, at < end && r.order ? r.order[at] : at, at < end);
 }
 
-// Sums over a row's entries: products in fp32, their sum in 64 bits, so that
-// long runs lose nothing and the order does not show.  Rows of at most MOST
+// Sums over a row's entries: products in fp32, their sum in 64 bits and one
+// rounding to fp32, so that long runs lose next to nothing.  The order of the
+// sum is fixed by the entries' places; another one could show where the exact
+// sum lies within 64 bits' error of a border of fp32.  Rows of at most MOST
 // lanes (below 64) take as few lanes as hold them, a power of two; 64 / lanes
 // groups add every so many entries each, and finish() adds the groups' sums.
 template <class TG, int MOST>
@@ -658,10 +668,13 @@ struct LongRun {
 // 64 / LANES at a time, where their runs are short; wider ones that one chunk
 // holds two at a time; the others one by one.
 // Narrow rows with 8-bit moments are held to the registers of five wavefronts
-// a SIMD: 264K entries of 192K rows of 100 columns 88 us, with four 96.
-// 156K rows of 400 (264K entries), 8-bit moments: 194 us; 14.4K rows (66K
-// entries) in 32 bits: 37 us, 3.7 TB/s.  The first is bound by the vector
+// a SIMD: 264K entries of 156K rows of 100 columns 88 us, with four 96.
+// 156K rows of 400 (264K entries), 8-bit moments: 191 us; 14.4K rows (66K
+// entries) in 32 bits: 36 us, 3.7 TB/s.  The first is bound by the vector
 // operations of k_adamw in 50 of 64 lanes, the second by the MALL.
+// SHORT is the most entries of a run that goes with others.  us with 2 / 4 / 6:
+// 264K entries of 156K rows of 100 95 / 88 / 93, of 58K rows 104 / 69 / 56; of
+// 156K rows of 400 193 / 191 / 192, of 58K rows 99 / 93 / 91.
 constexpr int SHORT = 4;
 template <class TP, class TG, int BITS, int LANES>
 __global__ __launch_bounds__(64, LANES < 64 && BITS == 8 ? 5 : 1) void k_adamw_rows(const RowsTensor r, const Hyper hyper, int window)
@@ -728,10 +741,13 @@ __global__ __launch_bounds__(64, LANES < 64 && BITS == 8 ? 5 : 1) void k_adamw_r
     }
     if (LANES == 64 && r.dim <= CHUNK) {
         // rows with few entries two at a time, so that the second's reads are
-        // on their way while the first is stepped: 194 us instead of 230 for the
-        // 156K rows, 9.1 ms instead of 9.9 for 7.9M rows of 86M, and 562 instead
-        // of 557 where most runs have three entries (one-by-one below that: pairs
-        // of single entries alone 203 and 601)
+        // on their way while the first is stepped, against one by one: 8-bit
+        // moments 191 instead of 230 us for the 156K rows, 4.8 ms instead of 5.4
+        // for 4.4M rows; in 32 bits, where it takes them from five wavefronts a
+        // SIMD to three, 36.5 instead of 38.1 for the 14.4K rows, 420 instead
+        // of 424 for the 156K, 360 instead of 369 at width 300.  It loses where
+        // there are few rows: 6,000 entries 16.8 against 16.2 us in 32 bits,
+        // 14.8 against 14.3 in 8.
         const uint64_t after = lane < 63 ? begins >> (lane + 1) : 0;
         const int mine = after ? __builtin_ctzll(after) + 1 : 64;      // entries of the run that begins here
         uint64_t quick = heads & __ballot(mine <= SHORT);
@@ -837,7 +853,10 @@ int dense_chunks(const smore_adamw_tensor* ts, int n, const Hyper& h, hipStream_
 template <class TP, class TG, int BITS>
 int dense_as(const smore_adamw_tensor* ts, int n, const Hyper& h, hipStream_t st, const char** err)
 {
-    // two chunks of a wavefront in flight, where that leaves enough wavefronts
+    // Two chunks of a wavefront in flight, where that leaves enough wavefronts.
+    // us with one / two: bf16 and 8-bit moments 4M elements 12.6 / 13.3, 32M 67.6
+    // / 65.3, 128M 283 / 276; fp32 4M 27.4 / 28.9, 16M 77 / 82, 32M 198 / 196,
+    // 128M 771 / 762.  Two lose with bf16 and 32-bit moments (128M 613 / 627).
     int64_t total = 0;
     for (int k = 0; k < n; ++k) total += ts[k].n_rows * ts[k].dim;
     if (total < (int64_t)CHUNK * WAVES * 4096) return dense_chunks<TP, TG, BITS, 1>(ts, n, h, st, err);

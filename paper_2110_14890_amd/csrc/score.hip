@@ -205,7 +205,8 @@ __global__ __launch_bounds__(64) void k_score(const TE* __restrict__ table, int6
 // their sums in LDS.  Several workgroups that share a query (splits > 1:
 // few queries with long lists) write partial sums, which k_join adds.
 // 4,096 x 257 candidates of 400,000 rows of 400 fp32: 197 us, 6.9 TB/s of
-// lines, the MALL's among them; 16 x 4,001 of width 200 in bf16: 8 + 3 us.
+// lines, the MALL's among them; 16 x 4,001 of width 200 in bf16: 9.4 us with
+// the sum of the parts.
 template <class TE, class TO, int LANES, int V, int NI, int U>
 __global__ __launch_bounds__(WG) void k_score_grad(const TE* __restrict__ table, int64_t table_stride, int rows, int dim,
                                                    const int32_t* __restrict__ ids, int64_t id_stride,
@@ -313,7 +314,10 @@ template <class TE, class TQ, int LANES, int V, int NI, int UNROLL>
 int score_as(const smore_score_args& a, const void* table, const void* queries, const int32_t* ids, float* scores,
              hipStream_t st, const char** err)
 {
-    // candidates per wavefront: up to 64, fewer where that leaves CUs without work
+    // Candidates per wavefront: up to 64, fewer where that leaves CUs without
+    // work.  us aimed at 2,048 / 4,096 / 8,192 wavefronts: 512 x 129 of width 400
+    // in fp32 20.3 / 20.2 / 19.2, 2,048 x 129 in bf16 39.1 / 39.1 / 40.8, 1 x
+    // 100,000 of width 200 11.0 / 10.6 / 12.5; 16 x 4,001 6.1 / 8.1 / 8.1.
     int tile = 64;
     while (tile > 8 && (int64_t)a.batch * ((a.n + tile - 1) / tile) < 4096) tile /= 2;
     const int tiles = (a.n + tile - 1) / tile;
@@ -337,7 +341,10 @@ int score_typed(const smore_score_args& a, const void* table, const void* querie
 }
 
 // Workgroups that share a query: enough to fill the chip, each wavefront
-// with at least 16 candidates.
+// with at least 16 candidates.  us aimed at 256 / 512 / 1,024 / 2,048 workgroups:
+// 16 x 4,001 of width 200 in bf16 10.9 / 9.4 / 9.1 / 9.0, 1 x 100,000 18.5 / 17.2 /
+// 19.1 / 26.3, 256 x 500 of width 400 26.5 / 23.7 / 24.1 / 24.9; 511 x 257 in
+// fp32 35.8 / 41.7 / 44.5 / 43.6.
 void grad_split(const smore_score_args& a, int* splits, int* span)
 {
     int64_t s = 1;

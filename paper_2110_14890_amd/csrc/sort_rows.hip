@@ -20,6 +20,8 @@ namespace {
 constexpr int WG = 256;
 constexpr int WAVES = WG / 64;
 constexpr int DIGITS = 256;
+// Tiles up to which each adds up the others' counts itself.  us with 16 / 64 /
+// 128: 33K entries 20.3 / 18.3 / 18.3, 66K 20.9 / 20.9 / 21.8, 131K 22 / 22 / 28.
 constexpr int FEW_TILES = 64;
 
 // Key of an id: the row, or the number of rows for one outside the table.
@@ -175,9 +177,11 @@ struct Plan {
         while (need < 32 && (1ll << need) <= n_rows) ++need;
         passes = (need + 7) / 8;
         bits = (need + passes - 1) / passes;
-        // us for 66K entries of 15,000 rows 23, 264K and 1.05M of 400,000 rows 41
-        // and 81, 8.4M of 86M rows 421
-        items = n <= (int64_t)1024 * WG * 4 ? 4 : 16;   // short tiles until they fill the chip
+        // Short tiles until they fill the chip.  us with 4 / 16 a thread: 66K
+        // entries of 15,000 rows 21 / 37, 264K and 1.05M of 400,000 rows 39 / 62
+        // and 67 / 80, 4.2M 185 / 151, 8.4M of 86M rows 470 / 433; equal at 2.1M,
+        // and in between 4 would still be better (1.1M 73 / 91).
+        items = n <= (int64_t)1024 * WG * 4 ? 4 : 16;
         tiles = (uint32_t)((n + WG * items - 1) / (WG * items));
         pairs = ((size_t)n * 4 + 255) & ~(size_t)255;
         counts = ((size_t)(tiles + 1) * DIGITS * 4 + 255) & ~(size_t)255;
