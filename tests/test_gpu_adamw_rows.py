@@ -83,3 +83,34 @@ def test_entries_add_up_to_one(dim, bits, param):
     assert np.array_equal(after[0], alone[0])
     for k in state:
         assert np.array_equal(after[1][k], alone[1][k]), (k, counts[(after[1][k] != alone[1][k]).any(1)])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dim,rows", [(24, 30_000), (200, 9_000), (400, 5_000)])
+def test_many_entries_add_up_to_one(dim, rows, bits):
+    """The same with more than 131,072 entries, of which a wavefront looks at
+    16 at a time: rows of one to 40 entries and a few of thousands, all bits
+    against the gradients given as one entry a row."""
+    import torch
+    rng = np.random.default_rng(dim)
+    dev = torch.device("cuda")
+    counts = rng.integers(1, 1 + 2 * 140_000 // rows, size=rows)
+    counts[rng.integers(0, rows, size=5)] = (1000, 128, 4096, 2500, 777)
+    ids = np.repeat(np.arange(rows), counts)
+    assert len(ids) > 131_072
+    # sums of at most 4,096 whole numbers of 12 bits
+    parts = torch.as_tensor(rng.integers(-2048, 2048, size=(len(ids), dim)), dtype=torch.float32, device=dev)
+    order = torch.as_tensor(rng.permutation(len(ids)), device=dev)
+    ids = torch.as_tensor(ids, device=dev)
+    total = torch.zeros((rows, dim), dtype=torch.float64, device=dev).index_add_(0, ids, parts.double())
+    p = torch.as_tensor(rng.normal(size=(rows, dim)) * 0.05, dtype=torch.bfloat16, device=dev)
+    q = p.clone()
+    kw = dict(OPT, bits=bits, seed=31, tables=(0,))
+    many, one = sm.AdamW([p], **kw), sm.AdamW([q], **kw)
+    for _ in range(2):
+        many.step([sm.row_grad(ids[order].int(), parts[order] * UNIT)])
+        one.step([sm.row_grad(torch.arange(rows, dtype=torch.int32, device=dev), (total * UNIT).float())])
+        assert torch.equal(p, q)
+        for k in many.states[0]:
+            a, b = [o.states[0][k].view(torch.uint8) for o in (many, one)]
+            assert torch.equal(a, b), k
