@@ -1019,8 +1019,9 @@ class AdamW:
 
         if stream is not None:
             kept += [grad_scale, self.lr if device_lr else None, self.device_steps]
+            names = ("m", "v", "m_scale", "v_scale") if scaled else ("m", "v")
             for k in used:
-                kept += [self.params[k], *self.states[k].values()]
+                kept += [self.params[k], *(self.states[k][n] for n in names)]
                 if type(grads[k]) is not RowGrad:
                     kept.append(grads[k])
         _check(_launch(device, stream, call, kept))

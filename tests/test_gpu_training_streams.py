@@ -147,3 +147,20 @@ def test_capture_on_a_given_stream():
         torch.cuda.synchronize()
         want = run(b, eager)
         assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(a, b), k
+
+
+def test_states_that_hold_more_than_moments():
+    """A checkpoint's state may carry other entries; a step on a given stream
+    looks at the moments alone, as one on the current stream does."""
+    import torch
+    p = torch.ones(300, device="cuda")
+    opt = sm.AdamW([p], lr=0.5, bits=8)
+    opt.states[0]["step"] = 7
+    opt.states[0]["note"] = None
+    g = torch.ones(300, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    opt.step([g], stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    opt.step([torch.ones(300, device="cuda")])
+    assert opt.steps == 2 and (p < 0.1).all()
