@@ -460,9 +460,9 @@ __device__ __forceinline__ void step_held(const Tensor& t, const Step& s, bool s
 __device__ __forceinline__ int left(int64_t end, int64_t at) { return (int)max((int64_t)0, min((int64_t)PER, end - at)); }
 
 // A workgroup takes WAVES x CHUNKS chunks of one tensor; which one it finds
-// among the launch's tensors by their first workgroups.  320M elements, bf16
+// among the launch's tensors by their first workgroups.  319M elements, bf16
 // parameters and gradients, 8-bit moments: 590 us, 5.5 TB/s, with vector
-// operations in 88 % of the issue slots (54 an element, a third of them the
+// operations in 90 % of the issue slots (53 an element, a third of them the
 // hash of the roundings); 15 tensors of 1.1M elements in 32 bits: 10 us.
 template <class TP, class TG, int BITS, int CHUNKS>
 __global__ __launch_bounds__(WG) void k_adamw(const TensorList list, const Hyper hyper)

@@ -61,8 +61,8 @@ __device__ __forceinline__ float across(float x, float* lds, int wave, F join)
 // blocks: rows of up to 64 x WAVES x V x STEPS scores stay in registers
 // between the sum and the gradient; longer ones are read again.  Gradients
 // are rounded once, to the scores' type.  16,384 x 512 in bf16 with reference
-// scores, softmax: 12.9 us (3.9 TB/s); 8,192 x 512 in fp32 with masks, pairs:
-// 11.5 us, one round of wavefronts; 64 x 16: 3.4 us, the launch.
+// scores, softmax: 13.2 us (3.8 TB/s); 8,192 x 512 in fp32 with masks, pairs:
+// 11.5 us, a third of the issue slots; 64 x 16: 3.6 us, the launch.
 template <class T, int WAVES, int V, int STEPS, bool SOFTMAX, bool REF, bool GRAD>
 __global__ __launch_bounds__(WG) void k_loss(const LossRow a)
 {
